@@ -112,6 +112,8 @@ typedef int o2m_status;
 #define O2M_ERR_SIZE (-25)      /* a padded size or plane offset exceeds the range  */
 #define O2M_ERR_SCALING (-26)   /* unknown scaling rule, or the Cauchy-Schwarz rule
                                    has no valid shifts for this n_moduli and k      */
+#define O2M_ERR_STEPS (-28)     /* o2m_orthogonalize: steps < 0 or > 64, no coef for
+                                   them, or an eps below zero or not finite        */
 #define O2M_ERR_SCRATCH (-27)   /* zgemm_2m_noalloc: the call needs more than
                                    O2M_NOALLOC_SCRATCH_BYTES of scratch memory      */
 
@@ -253,6 +255,114 @@ o2m_status zgemm_2m_residues(int m, int n, int k, const double *A, int lda, cons
 o2m_status zgemm_2m_residues_ex(int m, int n, int k, const double *A, int lda, const double *B,
                                 int ldb, int n_moduli, int scaling, int8_t *res, int32_t *E,
                                 int32_t *F, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Products of trained models: matrices held in 8-bit floating point with a
+ * scale for each block of 128, the linear layer made of them, and the
+ * orthogonalised update.
+ *
+ * These calls follow the conventions above (device pointers owned by the
+ * caller, stream, nothing synchronised, errors before anything is enqueued),
+ * with three differences:
+ *   - an 8-bit operand is a set of rows, each holding its k values of the inner
+ *     dimension contiguously (o2m_fp8_operand);
+ *   - scratch memory is the caller's: `workspace` of at least the bytes that the
+ *     call's ..._workspace function returns (0: none), 256-byte aligned, which
+ *     the call uses until the stream has passed it.  Calls that may overlap, and
+ *     graphs that may be replayed at the same time, need one each;
+ *   - no call allocates, so each can be captured into a graph at any time.
+ * ------------------------------------------------------------------------ */
+
+/* element types of unquantized matrices */
+#define O2M_TYPE_F32 0
+#define O2M_TYPE_F16 1
+#define O2M_TYPE_BF16 2
+
+/* 8-bit formats (OCP): largest numbers 448 and 57344 */
+#define O2M_FP8_E4M3 0
+#define O2M_FP8_E5M2 1
+
+/* kinds of scales: powers of two held as e8m0 bytes (exponent + 127; 255 is
+   NaN), or floats */
+#define O2M_SCALES_POW2 0
+#define O2M_SCALES_F32 1
+
+/* A matrix of `rows` x `k` values held in 8 bits: row r is k bytes at values + r
+   ld, with values 16-byte aligned and ld a multiple of 16, at least k.  The bytes
+   of a row past k are neither used nor written.  The value of entry (r, j) is
+   its 8-bit number times the scale of block (r / block, j / 128), which is
+   element (r / block) s_row + (j / 128) s_blk of scales. */
+typedef struct {
+    void *values;
+    int64_t ld;
+    void *scales;
+    int64_t s_row, s_blk;
+    int block;          /* rows of a block: 1 or 128 */
+    int format;         /* O2M_FP8_E4M3 or O2M_FP8_E5M2 */
+    int scale_type;     /* O2M_SCALES_POW2 or O2M_SCALES_F32 */
+} o2m_fp8_operand;
+
+/* X (rows x k, of x_type) into 8 bits: Q receives X (its rows hold k values),
+   Qt its transpose (k rows of `rows` values, quantized along those); either
+   may be NULL, and one call with both reads X once.  x_order 'R': entry (r, j)
+   at X[r ldx + j], 'C': at X[r + j ldx].  With amax the largest finite
+   magnitude of a block and F the largest number of its format,
+     POW2  s = 2^e, e the smallest integer >= -126 with amax <= F 2^e
+     F32   s = max(amax / F, 2^-126), rounded to nearest
+   (s = 1 when amax = 0), and an entry becomes fl(x fl(1/s)), limited to
+   [-F, F] and rounded to the nearest 8-bit number, ties to even; Inf and NaN
+   become NaN.  The blocks at the edges are shorter, nothing is written past
+   them.  Argument errors: -1 rows, -2 k, -3 X, -4 x_type, -5 x_order, -6 ldx,
+   -7 Q, -8 Qt. */
+o2m_status o2m_quantize_fp8(int rows, int k, const void *X, int x_type, char x_order, int64_t ldx,
+                            const o2m_fp8_operand *Q, const o2m_fp8_operand *Qt, void *stream);
+
+/* C = A B^T for 8-bit operands A (m rows of k) and B (n rows of k) of the same
+   kind of scales and any formats and blocks, rounded once to c_type.  For
+   fp32 results the products are exact and summed in fp32.  For 16-bit ones they are
+   summed by the 8-bit matrix unit, which adds 8 neighbouring products (k = 8 t
+   .. 8 t + 7) to within 2^-13 of the largest of them each, and these sums in
+   fp32: some 2e-5 of the result's norm, far below its rounding.  accumulate != 0: C += A B^T, the sum rounded once.  c_order 'R':
+   entry (i, j) at C[i ldc + j], 'C': at C[i + j ldc].  Rows holding NaN give
+   NaN.  k == 0: C is set to zero (accumulate: left as it is).  Every run
+   gives the same bits.  Argument errors: -1 m, -2 n, -3 k, -4 A, -5 B, -6 C,
+   -7 c_type, -8 c_order, -9 ldc. */
+o2m_status o2m_gemm_fp8(int m, int n, int k, const o2m_fp8_operand *A, const o2m_fp8_operand *B, void *C,
+                        int c_type, char c_order, int64_t ldc, int accumulate, void *workspace,
+                        size_t workspace_bytes, void *stream);
+size_t o2m_gemm_fp8_workspace(int m, int n, int k);
+
+/* The linear layer Y = X W^T: X (tokens x k, of x_type, row-major) is quantized
+   to e4m3 in blocks of 1 x 128 with W's kind of scales (as o2m_quantize_fp8
+   does) and multiplied with W (n rows of k); Y (tokens x n, row-major) is of
+   x_type.  One launch for few tokens.  Argument errors: -1 tokens, -2 n, -3 k,
+   -4 X, -5 x_type, -6 ldx, -7 W, -8 Y, -9 ldy. */
+o2m_status o2m_linear_fp8(int tokens, int n, int k, const void *X, int x_type, int64_t ldx,
+                          const o2m_fp8_operand *W, void *Y, int64_t ldy, void *workspace,
+                          size_t workspace_bytes, void *stream);
+size_t o2m_linear_fp8_workspace(int tokens, int n, int k);
+
+/* The orthogonalised update: for each of `batch` matrices G (rows x cols, of
+   type, matrix b at G + b stride_g)
+     X = G / (||G|| + eps)   (Frobenius norm),
+     `steps` times  X <- a X + (b A + c A^2) X  with A = X X^T,
+   (a, b, c) = coef[3 t .. 3 t + 2] in step t (host memory), and X is written to
+   O, of the same type; transposed where rows > cols, which is the same X.
+   order 'R': entry (i, j) at i ld + j, 'C': at i + j ld, for G and O each.  The
+   norm is summed in fp64 and products in fp32; between products bf16 matrices
+   are held in fp16 with one power-of-two scale (11 bits, 3 more than the
+   result), fp32 and fp16 ones in two fp16 parts (22 bits).  The held range
+   asks for singular values below 16 in every step, which the usual
+   coefficients keep far below 2.  Inf or NaN in G gives NaN in the whole
+   matrix.  O must not overlap G, except to be G in the same layout.  Argument
+   errors: -1 batch, -2 rows, -3 cols, -4 G, -5 order_g, -6 ldg, -7 stride_g,
+   -8 O, -9 order_o, -10 ldo, -11 stride_o, -12 type, O2M_ERR_STEPS steps,
+   coef or eps. */
+o2m_status o2m_orthogonalize(int batch, int rows, int cols, const void *G, char order_g, int64_t ldg,
+                             int64_t stride_g, void *O, char order_o, int64_t ldo, int64_t stride_o, int type,
+                             int steps, const double *coef, double eps, void *workspace,
+                             size_t workspace_bytes, void *stream);
+size_t o2m_orthogonalize_workspace(int batch, int rows, int cols, int type);
 
 /* Host-only: the first n_moduli moduli (1..32: the 2M moduli of Section 4,
    then the hybrid 3M extension), the smallest square roots of -1 of the 2M

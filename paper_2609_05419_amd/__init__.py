@@ -9,6 +9,9 @@ package raises.
 Matrices are column-major: a tensor ``A`` of shape (m, k) must have
 ``A.stride(0) == 1`` (``colmajor(x)`` makes such a tensor).  Outputs are
 allocated column-major as well.
+
+The products of trained models (8-bit block-scaled matrices, the linear layer,
+the orthogonalised update) are in ``model_ops``.
 """
 from __future__ import annotations
 
@@ -22,6 +25,7 @@ __all__ = [
     "zher2k_2m", "dsyr2k_2m", "gauss_gemm_2m",
     "zgemm_2m_residues", "moduli", "budget", "shifts", "workspace_bytes", "set_workspace",
     "release_workspace", "get_status", "STATUS_OVERFLOW", "STATUS_NONFINITE", "phase_timing", "phase_times", "colmajor", "O2MError", "LIB_PATH", "SCALING",
+    "Fp8Operand", "quantize_fp8", "quantize_fp8_pair", "gemm_fp8", "linear_fp8", "linear_fp8_backward", "orthogonalize",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libo2m.so")
@@ -402,3 +406,7 @@ def phase_times() -> dict:
     if n < 0:
         raise RuntimeError("o2m_phase_times failed")
     return {PHASES[i]: float(buf[i]) for i in range(n)}
+
+
+from .model_ops import (Fp8Operand, gemm_fp8, linear_fp8, linear_fp8_backward, orthogonalize, quantize_fp8,  # noqa: E402
+                        quantize_fp8_pair)

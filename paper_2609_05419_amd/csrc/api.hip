@@ -836,6 +836,7 @@ const char *o2m_status_string(o2m_status s) {
     case O2M_ERR_SIZE: return "problem too large for the tile grid";
     case O2M_ERR_SCALING: return "unknown scaling rule, or no Cauchy-Schwarz shifts for this n_moduli and k";
     case O2M_ERR_SCRATCH: return "zgemm_2m_noalloc: the call needs more than the static scratch array (O2M_NOALLOC_SCRATCH_BYTES)";
+    case O2M_ERR_STEPS: return "o2m_orthogonalize: steps outside 0..64, no coefficients for them, or an eps below zero or not finite";
     default: break;
     }
     if (s < 0 && s >= -12) return "invalid argument (BLAS position = -status)";

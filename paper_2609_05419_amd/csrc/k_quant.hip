@@ -1,0 +1,255 @@
+// Quantization into 8-bit floating point with a scale for each block of 1 x
+// 128 or 128 x 128 entries (include/o2m.h: o2m_quantize_fp8).
+//
+// Bound: memory.  One read of X and one write of each operand.
+#include "model_internal.h"
+
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+#include <type_traits>
+
+namespace o2m {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+struct Dest {
+    uint8_t *values;
+    int64_t ld;
+    void *scales;
+    int64_t s_row, s_blk;
+    int block, format, scale_type;
+};
+
+struct QuantArgs {
+    const void *X;
+    int64_t ld;
+    int lines, len;
+    int tiles_q;      // tiles along a line
+    Dest along, across;
+};
+
+__device__ inline float as_float(float x) { return x; }
+__device__ inline float as_float(__half x) { return __half2float(x); }
+__device__ inline float as_float(__hip_bfloat16 x) { return __bfloat162float(x); }
+
+__device__ inline bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+// |x|, and 0 in the place of Inf and NaN
+__device__ inline float magnitude(float x) { return finite(x) ? fabsf(x) : 0.0f; }
+
+// A block's scale: its inverse in fp32, and what the operand holds (the float's
+// bits, or exponent + 127).
+struct Scale {
+    float inv;
+    uint32_t held;
+};
+__device__ inline Scale scale_of(float amax, int format, int scale_type) {
+    if (scale_type == O2M_SCALES_F32) {
+        const float top = format == O2M_FP8_E4M3 ? 448.0f : 57344.0f;
+        const float s = amax > 0.0f ? fmaxf(__fdiv_rn(amax, top), 1.17549435e-38f) : 1.0f;
+        return {__fdiv_rn(1.0f, s), __float_as_uint(s)};
+    }
+    // F = 1.75 2^p: the exponent of amax less p, and one more past 1.75
+    const uint32_t bits = __float_as_uint(amax);
+    const int p = format == O2M_FP8_E4M3 ? 8 : 15;
+    int e = (int)(bits >> 23) - 127 - p + ((bits & 0x7FFFFFu) > 0x600000u);
+    e = amax > 0.0f ? max(e, -126) : 0;
+    return {__uint_as_float((uint32_t)(127 - e) << 23), (uint32_t)(e + 127)};
+}
+
+__device__ inline void store_scale(const Dest &d, int64_t row, int64_t blk, uint32_t held) {
+    const int64_t i = row * d.s_row + blk * d.s_blk;
+    if (d.scale_type == O2M_SCALES_F32) static_cast<uint32_t *>(d.scales)[i] = held;
+    else static_cast<uint8_t *>(d.scales)[i] = (uint8_t)held;
+}
+
+// x inv within the format's range; Inf and NaN become NaN.
+__device__ inline float scaled(float x, float inv, float top) {
+    const float y = fminf(fmaxf(x * inv, -top), top);
+    return finite(x) ? y : __uint_as_float(0x7FC00000u);
+}
+
+// Four values in 8 bits, rounded to nearest, ties to even.
+__device__ inline uint32_t pack_fp8(const float (&y)[4], int format) {
+    int r = 0;
+    if (format == O2M_FP8_E4M3) {
+        r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], r, false);
+        r = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
+    } else {
+        r = __builtin_amdgcn_cvt_pk_bf8_f32(y[0], y[1], r, false);
+        r = __builtin_amdgcn_cvt_pk_bf8_f32(y[2], y[3], r, true);
+    }
+    return (uint32_t)r;
+}
+
+// Eight entries of one line from `x0`, of which `n` exist; zeros after them.
+template <class T, bool VEC>
+__device__ inline void load8(const T *x0, int n, float (&v)[8]) {
+    if (VEC && n >= 8) {
+        T t[8];
+        constexpr int parts = sizeof(T) * 8 / 16;
+#pragma unroll
+        for (int i = 0; i < parts; ++i)
+            reinterpret_cast<u32x4 *>(t)[i] = reinterpret_cast<const u32x4 *>(x0)[i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = as_float(t[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? as_float(x0[j]) : 0.0f;
+    }
+}
+
+__device__ inline void store_bytes(uint8_t *p, uint2 w, int n) {
+    if (n >= 8) {
+        *reinterpret_cast<uint2 *>(p) = w;
+    } else {
+        for (int j = 0; j < n; ++j) p[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    }
+}
+
+// One tile of 128 x 128 entries per workgroup, quantized along its lines, across
+// them or both.  Thread (rg, cg) holds the 8 x 8 entries of lines 8 rg.. and
+// positions 8 cg..: 16 threads share a line, whose maximum is taken by lane
+// exchanges, and the maxima across lines and the bytes of the transposed operand
+// go through LDS (in 8-byte units of 8 lines, unit rg of position q in slot rg ^
+// (q / 8), which spreads both the writes and the reads over the banks).
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void quantize_tile(QuantArgs g) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[128 * 128];
+    __shared__ float tile_max[4];
+    const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
+    const int tp = blockIdx.x / g.tiles_q, tq = blockIdx.x % g.tiles_q;
+    const int p0 = tp * 128 + 8 * rg, q0 = tq * 128 + 8 * cg;
+    const int nq = min(8, g.len - q0);
+    float x[8][8], row_max[8], col_max[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) col_max[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        load8<T, VEC>(static_cast<const T *>(g.X) + (int64_t)(p0 + i) * g.ld + q0, p0 + i < g.lines ? nq : 0, x[i]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float a = magnitude(x[i][j]);
+            m = fmaxf(m, a);
+            col_max[j] = fmaxf(col_max[j], a);
+        }
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+        row_max[i] = m;
+    }
+    const bool whole = g.along.block == kBlockK || g.across.block == kBlockK;
+    float all = 0.0f;
+    if (whole) {   // (uniform over the workgroup)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) all = fmaxf(all, row_max[i]);
+        all = fmaxf(all, __shfl_xor(all, 16));
+        all = fmaxf(all, __shfl_xor(all, 32));
+        if ((tid & 63) == 0) tile_max[tid >> 6] = all;
+        __syncthreads();
+        all = fmaxf(fmaxf(tile_max[0], tile_max[1]), fmaxf(tile_max[2], tile_max[3]));
+    }
+
+    if (g.along.values) {
+        const Dest &d = g.along;
+        const float top = d.format == O2M_FP8_E4M3 ? 448.0f : 57344.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const Scale s = scale_of(d.block == 1 ? row_max[i] : all, d.format, d.scale_type);
+            if (p0 + i >= g.lines || nq <= 0) continue;
+            float y[4], z[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                y[j] = scaled(x[i][j], s.inv, top);
+                z[j] = scaled(x[i][4 + j], s.inv, top);
+            }
+            store_bytes(d.values + (int64_t)(p0 + i) * d.ld + q0, uint2{pack_fp8(y, d.format), pack_fp8(z, d.format)}, nq);
+            if (cg == 0 && d.block == 1) store_scale(d, p0 + i, tq, s.held);
+            if (tid == 0 && i == 0 && d.block == kBlockK) store_scale(d, tp, tq, s.held);
+        }
+    }
+
+    if (g.across.values) {
+        const Dest &d = g.across;
+        const float top = d.format == O2M_FP8_E4M3 ? 448.0f : 57344.0f;
+        Scale s[8];
+        if (d.block == 1) {
+            float *part = reinterpret_cast<float *>(lds);   // [16][128]
+#pragma unroll
+            for (int j = 0; j < 8; ++j) part[rg * 128 + 8 * cg + j] = col_max[j];
+            __syncthreads();
+            float m = 0.0f;
+            if (tid < 128) {
+                for (int r = 0; r < 16; ++r) m = fmaxf(m, part[r * 128 + tid]);
+            }
+            __syncthreads();
+            if (tid < 128) part[tid] = m;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s[j] = scale_of(part[8 * cg + j], d.format, d.scale_type);
+                if (rg == 0 && j < nq) store_scale(d, q0 + j, tp, s[j].held);
+            }
+            __syncthreads();   // before the bytes overwrite the maxima
+        } else {
+            const Scale t = scale_of(all, d.format, d.scale_type);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] = t;
+            if (tid == 0) store_scale(d, tq, tp, t.held);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float y[4], z[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[i] = scaled(x[i][j], s[j].inv, top);
+                z[i] = scaled(x[4 + i][j], s[j].inv, top);
+            }
+            *reinterpret_cast<uint2 *>(lds + (8 * cg + j) * 128 + ((rg ^ cg) << 3)) =
+                uint2{pack_fp8(y, d.format), pack_fp8(z, d.format)};
+        }
+        __syncthreads();
+        // unit u (8 lines) of position q: 16 consecutive threads write the 128
+        // bytes of one operand row
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int q = 16 * i + (tid >> 4), u = tid & 15;
+            const uint2 w = *reinterpret_cast<const uint2 *>(lds + q * 128 + ((u ^ (q >> 3)) << 3));
+            const int line = tp * 128 + 8 * u;
+            if (tq * 128 + q < g.len && line < g.lines)
+                store_bytes(d.values + (int64_t)(tq * 128 + q) * d.ld + line, w, min(8, g.lines - line));
+        }
+    }
+}
+
+Dest dest_of(const o2m_fp8_operand *o) {
+    if (!o) return {nullptr, 0, nullptr, 0, 0, 0, 0, 0};
+    return {static_cast<uint8_t *>(o->values), o->ld, o->scales, o->s_row, o->s_blk, o->block, o->format, o->scale_type};
+}
+
+template <class T>
+void launch_tiles(const QuantArgs &g, unsigned grid, hipStream_t st) {
+    const bool vec = (reinterpret_cast<uintptr_t>(g.X) % 16 == 0) && (g.ld * (int64_t)sizeof(T)) % 16 == 0;
+    if (vec) quantize_tile<T, true><<<grid, 256, 0, st>>>(g);
+    else quantize_tile<T, false><<<grid, 256, 0, st>>>(g);
+}
+
+}  // namespace
+
+hipError_t launch_quantize(int lines, int len, const void *X, int type, int64_t ld, const o2m_fp8_operand *along,
+                           const o2m_fp8_operand *across, hipStream_t st) {
+    const int64_t tiles_q = ceil_div(len, 128), tiles = tiles_q * ceil_div(lines, 128);
+    if (tiles <= 0) return hipSuccess;
+    if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
+    const QuantArgs g = {X, ld, lines, len, (int)tiles_q, dest_of(along), dest_of(across)};
+    switch (type) {
+    case O2M_TYPE_F32: launch_tiles<float>(g, (unsigned)tiles, st); break;
+    case O2M_TYPE_F16: launch_tiles<__half>(g, (unsigned)tiles, st); break;
+    default: launch_tiles<__hip_bfloat16>(g, (unsigned)tiles, st); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace o2m

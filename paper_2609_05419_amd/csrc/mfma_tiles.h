@@ -1,0 +1,80 @@
+// What the product kernels of k_fp8.hip and k_ortho.hip share: operand rows
+// staged through LDS in k-stages of 128 bytes (128 8-bit or 64 16-bit values),
+// and the 16-row fragments that the MFMAs read from there.
+//
+// A stage of R rows is R x 128 bytes of LDS, row after row.  It arrives by
+// direct buffer->LDS copies of 1 KB per wave: 8 rows, each a whole 128-byte
+// line of its operand.  The 16-byte chunk c of row r lies in slot c ^ (r & 7)
+// of its row, so that the lanes of a fragment read, which take one chunk of 16
+// different rows, spread over all banks.  The swizzle costs nothing: a copy's
+// destination is fixed (lane x 16), its source address is each lane's own.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace o2m {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_ptr;
+
+constexpr int kStageRowBytes = 128;
+constexpr int kFragRowCount = 16;
+
+// s_waitcnt on the vector-memory counter only (gfx9 encoding), n <= 63
+template <int N>
+__device__ inline void wait_vmem() {
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (0xF << 8));
+}
+
+// Workgroup barrier that leaves copies in flight: this wave's LDS reads have
+// returned (lgkmcnt 0), its copies are waited for by wait_vmem beforehand.
+__device__ inline void lds_barrier() {
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Descriptor of `rows` operand rows of kbytes each, `ld` bytes apart: reads
+// past the last one give zeros.  ld < 2^23 (checked on the host) keeps every
+// offset of a tile below 2^31.
+__device__ inline __amdgpu_buffer_rsrc_t rows_of(const uint8_t *base, int rows, int64_t ld, int kbytes) {
+    const int extent = rows > 0 ? (int)((rows - 1) * ld) + ((kbytes + 15) & ~15) : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), (short)0, extent, 0x00020000);
+}
+
+// One lane's part of a copy: its row (of 8) and the chunk that its slot holds.
+struct CopyLane {
+    int row, chunk16;   // chunk16: byte offset of the chunk within the stage row
+};
+__device__ inline CopyLane copy_lane(int lane) {
+    return {lane >> 3, ((lane & 7) ^ (lane >> 3)) * 16};
+}
+
+// Copy rows [8 q, 8 q + 8) of stage kb to dst (wave-uniform, 1 KB).  `left` is
+// the operand's bytes from this stage on: chunks past it are read as zeros.
+__device__ inline void copy_rows(__amdgpu_buffer_rsrc_t r, uint8_t *dst, CopyLane c, int q, int ld, int kb, int left) {
+    int off = (8 * q + c.row) * ld + c.chunk16;
+    if (left < kStageRowBytes) off = c.chunk16 < left ? off : 0x7FFFFFF0;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr *)dst, 16, off, kb * kStageRowBytes, 0, 0);
+}
+
+// Zero the bytes of row `row` past `left` in the chunk that holds byte `left`.
+__device__ inline void clear_row_tail(uint8_t *stage, int row, int left) {
+    uint8_t *chunk = stage + row * kStageRowBytes + (((left >> 4) ^ (row & 7)) << 4);
+    for (int b = left & 15; b < 16; ++b) chunk[b] = 0;
+}
+
+// The 32 bytes of a fragment that one lane holds: row lane % 16 of the 16, bytes
+// [32 g, 32 g + 32) of the stage row with g = lane / 16.
+__device__ inline v8i read_fragment(const uint8_t *stage, int row0, int lane) {
+    const int row = row0 + (lane & 15), c = 2 * (lane >> 4);
+    const uint8_t *p = stage + row * kStageRowBytes;
+    const int4 lo = *reinterpret_cast<const int4 *>(p + ((c ^ (row & 7)) << 4));
+    const int4 hi = *reinterpret_cast<const int4 *>(p + (((c + 1) ^ (row & 7)) << 4));
+    return v8i{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+}
+
+}  // namespace o2m

@@ -1,0 +1,48 @@
+// Internal definitions of the products of trained models: 8-bit block-scaled
+// operands (o2m_fp8_operand, include/o2m.h) and the orthogonalised update.
+// What the product kernels share (staging of operand rows through LDS, the
+// MFMA fragments) is in mfma_tiles.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "o2m.h"
+
+namespace o2m {
+
+constexpr int kBlockK = 128;   // entries of a block along the inner dimension
+
+inline int64_t ceil_div(int64_t x, int64_t q) { return (x + q - 1) / q; }
+inline int64_t round_up64(int64_t x, int64_t q) { return ceil_div(x, q) * q; }
+
+// Quantize the matrix of `lines` x `len` entries, entry (p, q) at X[p ld + q]:
+// along its lines into `along` and across them into `across` (rows of an
+// operand are lines, or entry positions q); either may be null.
+hipError_t launch_quantize(int lines, int len, const void *X, int type, int64_t ld, const o2m_fp8_operand *along,
+                           const o2m_fp8_operand *across, hipStream_t st);
+
+// C = A B^T with C's m contiguous: entry (i, j) at C[i + j ldc].
+hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const o2m_fp8_operand &B, void *C, int type,
+                           int64_t ldc, bool accumulate, void *ws, hipStream_t st);
+size_t gemm_fp8_workspace(int m, int n, int k);
+
+struct OrthoArgs {
+    int batch, rows, cols;          // of the work matrix: rows <= cols
+    const void *G;
+    int64_t g_row, g_col, g_batch;  // strides in elements
+    void *O;
+    int64_t o_row, o_col, o_batch;
+    int type;
+    int steps;
+    const double *coef;
+    double eps;
+};
+size_t ortho_workspace(int batch, int rows, int cols, int type);
+hipError_t launch_ortho(const OrthoArgs &g, void *ws, hipStream_t st);
+
+// Zero entries (i, j) of C at i + j ldc, of `size` bytes.
+hipError_t launch_zero_out(void *C, int64_t m, int64_t n, int64_t ldc, int size, hipStream_t st);
+
+}  // namespace o2m

@@ -1,0 +1,320 @@
+"""Products of trained models on MI355X: matrices held in 8-bit floating point
+with a scale for each block of 128, the linear layer made of them, and the
+orthogonalised update.
+
+Thin binding, as the package's other calls: every step runs in the library's
+HIP kernels, enqueued on the current stream (or ``stream``); nothing is
+synchronised, and without the library the import fails.  Tensors live on the
+current device.  Outputs and scratch memory come from torch's allocator, from
+the pool of the stream that uses them, so that calls on different streams and
+captured graphs share none.
+
+An 8-bit operand is a pair ``(values, scales)``: ``values`` of shape (rows, k)
+in ``torch.float8_e4m3fn`` or ``torch.float8_e5m2``, k running contiguously and
+rows starting at multiples of 16 bytes, ``scales`` of shape (rows, ceil(k /
+128)) for blocks of 1 x 128 or (ceil(rows / 128), ceil(k / 128)) for blocks of
+128 x 128, in ``torch.float8_e8m0fnu`` (powers of two) or ``torch.float32``.  The
+matrix it stands for is each value times its block's scale.  ``quantize_fp8``
+makes one.  Other matrices may be row-major or column-major.  There is no
+autograd here: the backward products are calls of their own.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple
+
+import torch
+
+from . import _L, _check, _stream
+
+__all__ = ["Fp8Operand", "quantize_fp8", "quantize_fp8_pair", "gemm_fp8", "linear_fp8", "linear_fp8_backward",
+           "orthogonalize"]
+
+_I, _L64, _P, _D, _C, _Z = (ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_double, ctypes.c_char,
+                            ctypes.c_size_t)
+
+
+class _Operand(ctypes.Structure):
+    _fields_ = [("values", _P), ("ld", _L64), ("scales", _P), ("s_row", _L64), ("s_blk", _L64), ("block", _I),
+                ("format", _I), ("scale_type", _I)]
+
+
+_O = ctypes.POINTER(_Operand)
+_L.o2m_quantize_fp8.argtypes = [_I, _I, _P, _I, _C, _L64, _O, _O, _P]
+_L.o2m_gemm_fp8.argtypes = [_I, _I, _I, _O, _O, _P, _I, _C, _L64, _I, _P, _Z, _P]
+_L.o2m_linear_fp8.argtypes = [_I, _I, _I, _P, _I, _L64, _O, _P, _L64, _P, _Z, _P]
+_L.o2m_orthogonalize.argtypes = [_I, _I, _I, _P, _C, _L64, _L64, _P, _C, _L64, _L64, _I, _I, _P, _D, _P, _Z, _P]
+for _f in ("o2m_quantize_fp8", "o2m_gemm_fp8", "o2m_linear_fp8", "o2m_orthogonalize"):
+    getattr(_L, _f).restype = _I
+_L.o2m_gemm_fp8_workspace.argtypes = [_I, _I, _I]
+_L.o2m_linear_fp8_workspace.argtypes = [_I, _I, _I]
+_L.o2m_orthogonalize_workspace.argtypes = [_I, _I, _I, _I]
+for _f in ("o2m_gemm_fp8_workspace", "o2m_linear_fp8_workspace", "o2m_orthogonalize_workspace"):
+    getattr(_L, _f).restype = _Z
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_FORMATS = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+_SCALES = {"pow2": 0, "float32": 1}
+_SCALE_DTYPES = {"pow2": torch.float8_e8m0fnu, "float32": torch.float32}
+BLOCK = 128
+
+
+class Fp8Operand(NamedTuple):
+    """A matrix held in 8 bits: values (rows, k) and the scales of its blocks."""
+    values: torch.Tensor
+    scales: torch.Tensor
+
+
+def _here(x: torch.Tensor, name: str) -> None:
+    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a tensor on the current device")
+
+
+def _type_of(x: torch.Tensor, name: str) -> int:
+    t = _TYPES.get(x.dtype)
+    if t is None:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {x.dtype}")
+    return t
+
+
+def _order(rows: int, cols: int, s0: int, s1: int, name: str):
+    """(order, leading dimension) of a rows x cols matrix with these strides."""
+    if rows <= 1 or cols <= 1 or rows * cols == 0:
+        if rows * cols == 0 or (cols <= 1 and rows <= 1):
+            return b"R", max(cols, 1)
+        if cols == 1:
+            return b"R", max(s0, 1)              # entry i at i s0
+        return (b"R", cols) if s1 == 1 else (b"C", max(s1, 1))
+    if s1 == 1:
+        return b"R", s0
+    if s0 == 1:
+        return b"C", s1
+    raise ValueError(f"{name} must be row-major or column-major")
+
+
+def _matrix(x: torch.Tensor, name: str):
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be a matrix, got {x.dim()} dimensions")
+    _here(x, name)
+    return _order(x.size(0), x.size(1), x.stride(0), x.stride(1), name)
+
+
+def _operand(x, name: str) -> _Operand:
+    """The C struct of an 8-bit operand, its shapes and types checked."""
+    q, s = x
+    fmt = _FORMATS.get(q.dtype)
+    if fmt is None:
+        raise TypeError(f"{name}: values must be float8_e4m3fn or float8_e5m2, got {q.dtype}")
+    if q.dim() != 2 or s.dim() != 2:
+        raise ValueError(f"{name}: values and scales must be matrices")
+    _here(q, name)
+    _here(s, name)
+    if s.dtype == torch.float32:
+        kind = 1
+    elif s.dtype == torch.float8_e8m0fnu or s.dtype == torch.uint8:
+        kind = 0
+    else:
+        raise TypeError(f"{name}: scales must be float8_e8m0fnu (or its bytes) or float32, got {s.dtype}")
+    rows, k = q.shape
+    if k > 1 and rows > 0 and q.stride(1) != 1:
+        raise ValueError(f"{name}: the k values of a row must be contiguous (stride(1) == 1)")
+    ld = q.stride(0) if rows > 1 and k > 0 else (k + 15) // 16 * 16
+    if ld % 16 or q.data_ptr() % 16 or ld < k:
+        raise ValueError(f"{name}: rows must start at multiples of 16 bytes, one after another")
+    if s.size(1) != (k + BLOCK - 1) // BLOCK:
+        raise ValueError(f"{name}: {k} values a row need {(k + BLOCK - 1) // BLOCK} columns of scales, got {s.size(1)}")
+    if s.size(0) == rows:
+        block = 1
+    elif s.size(0) == (rows + BLOCK - 1) // BLOCK:
+        block = BLOCK
+    else:
+        raise ValueError(f"{name}: {rows} rows need {rows} or {(rows + BLOCK - 1) // BLOCK} rows of scales, "
+                         f"got {s.size(0)}")
+    return _Operand(q.data_ptr(), ld, s.data_ptr(), s.stride(0), s.stride(1), block, fmt, kind)
+
+
+def _empty(size, dtype, device, stream):
+    """Memory of the pool of the stream that will use it."""
+    if stream is None:
+        return torch.empty(size, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(size, dtype=dtype, device=device)
+
+
+def _scratch(nbytes: int, device, stream):
+    """(tensor that holds it, address, bytes) of scratch memory; torch's blocks
+    are 512-byte aligned."""
+    if nbytes == 0:
+        return None, None, 0
+    t = _empty((nbytes,), torch.uint8, device, stream)
+    return t, t.data_ptr(), nbytes
+
+
+def _fresh_operand(rows: int, k: int, block: int, dtype, scales: str, device, stream) -> Fp8Operand:
+    q = _empty((rows, (k + 15) // 16 * 16), torch.uint8, device, stream)[:, :k].view(dtype)
+    r, kb = (rows if block == 1 else (rows + BLOCK - 1) // BLOCK), (k + BLOCK - 1) // BLOCK
+    s = _empty((kb, r), torch.uint8 if scales == "pow2" else torch.float32, device, stream)
+    return Fp8Operand(q, (s.view(torch.float8_e8m0fnu) if scales == "pow2" else s).t())
+
+
+def _quantize_args(block, dtype, scales):
+    if tuple(block) not in ((1, BLOCK), (BLOCK, BLOCK)):
+        raise ValueError(f"block must be (1, 128) or (128, 128), got {block!r}")
+    if dtype not in _FORMATS:
+        raise TypeError(f"dtype must be float8_e4m3fn or float8_e5m2, got {dtype}")
+    if scales not in _SCALES:
+        raise ValueError(f"unknown kind of scales {scales!r}; expected one of {sorted(_SCALES)}")
+    return block[0]
+
+
+def _quantize(X, Q, Qt, name, stream):
+    t = _type_of(X, "X")
+    order, ld = _matrix(X, "X")
+    rows, k = X.shape
+    structs = []
+    for what, x, shape in (("out", Q, (rows, k)), ("transposed out", Qt, (k, rows))):
+        if x is None:
+            structs.append(None)
+            continue
+        if tuple(x[0].shape) != shape:
+            raise ValueError(f"{what}: values must be of shape {shape}, got {tuple(x[0].shape)}")
+        structs.append(ctypes.byref(_operand(x, what)))
+    _check(_L.o2m_quantize_fp8(rows, k, X.data_ptr(), t, order, ld, structs[0], structs[1], _stream(stream)), name)
+
+
+def quantize_fp8(X: torch.Tensor, block=(1, 128), dtype=torch.float8_e4m3fn, scales: str = "pow2", out=None,
+                 stream=None) -> Fp8Operand:
+    """X (rows x k, float32, float16 or bfloat16) as an 8-bit operand: blocks of
+    1 x 128 or 128 x 128, the last ones shorter.
+
+    With amax the largest finite magnitude of a block and F the format's largest
+    number, ``scales="pow2"`` takes the smallest power of two s >= amax / F (from
+    2^-126), ``"float32"`` s = amax / F; entries become x (1 / s), rounded to
+    nearest, ties to even, and Inf and NaN become NaN.  ``quantize_fp8(X.t())``
+    is the operand of the transpose.  ``out``: an operand to write into, of any
+    format and kind of scales (the other arguments are then not used)."""
+    if out is None:
+        b = _quantize_args(block, dtype, scales)
+        out = _fresh_operand(X.size(0), X.size(1), b, dtype, scales, X.device, stream) if X.dim() == 2 else out
+    _quantize(X, out, None, "quantize_fp8", stream)
+    return out
+
+
+def quantize_fp8_pair(X: torch.Tensor, block=(1, 128), dtype=torch.float8_e4m3fn, scales: str = "pow2", out=None,
+                      stream=None) -> tuple[Fp8Operand, Fp8Operand]:
+    """The operands of X and of its transpose from one reading of X (what a
+    layer's forward product and its backward products take of X, W or dY).
+    ``out``: a pair of operands to write into."""
+    if out is None:
+        b = _quantize_args(block, dtype, scales)
+        if X.dim() != 2:
+            raise ValueError(f"X must be a matrix, got {X.dim()} dimensions")
+        rows, k = X.shape
+        out = (_fresh_operand(rows, k, b, dtype, scales, X.device, stream),
+               _fresh_operand(k, rows, b, dtype, scales, X.device, stream))
+    _quantize(X, out[0], out[1], "quantize_fp8_pair", stream)
+    return out
+
+
+def gemm_fp8(A, B, dtype=torch.bfloat16, out: torch.Tensor | None = None, accumulate: bool = False,
+             stream=None) -> torch.Tensor:
+    """C = A B^T for 8-bit operands A (m rows of k) and B (n rows of k) of one
+    kind of scales and any formats and blocks; summed in fp32, rounded once to
+    ``dtype`` (or that of ``out``, which may be row-major or column-major).
+    ``accumulate``: out += A B^T, rounded once."""
+    a, b = _operand(A, "A"), _operand(B, "B")
+    m, k = A[0].shape
+    n = B[0].size(0)
+    if B[0].size(1) != k:
+        raise ValueError(f"inner dimensions differ: {tuple(A[0].shape)} and {tuple(B[0].shape)}")
+    if a.scale_type != b.scale_type:
+        raise TypeError("A and B must have the same kind of scales")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        if dtype not in _TYPES:
+            raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+        out = _empty((m, n), dtype, A[0].device, stream)
+    elif tuple(out.shape) != (m, n):
+        raise ValueError(f"out must be of shape {(m, n)}, got {tuple(out.shape)}")
+    t = _type_of(out, "out")
+    order, ld = _matrix(out, "out")
+    ws, at, nbytes = _scratch(_L.o2m_gemm_fp8_workspace(m, n, k), out.device, stream)
+    _check(_L.o2m_gemm_fp8(m, n, k, ctypes.byref(a), ctypes.byref(b), out.data_ptr(), t, order, ld, int(accumulate), at,
+                           nbytes, _stream(stream)), "gemm_fp8")
+    return out
+
+
+def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The linear layer Y = X W^T: X (tokens x k, row-major) is quantized to e4m3
+    in blocks of 1 x 128 with W's kind of scales and multiplied with the operand
+    W (n rows of k); Y (tokens x n, row-major) has X's type."""
+    w = _operand(W, "W")
+    t = _type_of(X, "X")
+    order, ldx = _matrix(X, "X")
+    tokens, k = X.shape
+    n = W[0].size(0)
+    if W[0].size(1) != k:
+        raise ValueError(f"inner dimensions differ: {tuple(X.shape)} and {tuple(W[0].shape)}")
+    if order != b"R":
+        raise ValueError("X must be row-major")
+    if out is None:
+        out = _empty((tokens, n), X.dtype, X.device, stream)
+    elif tuple(out.shape) != (tokens, n) or out.dtype != X.dtype:
+        raise ValueError(f"out must be {X.dtype} of shape {(tokens, n)}")
+    order, ldy = _matrix(out, "out")
+    if order != b"R":
+        raise ValueError("out must be row-major")
+    ws, at, nbytes = _scratch(_L.o2m_linear_fp8_workspace(tokens, n, k), out.device, stream)
+    _check(_L.o2m_linear_fp8(tokens, n, k, X.data_ptr(), t, ldx, ctypes.byref(w), out.data_ptr(), ldy, at, nbytes,
+                             _stream(stream)), "linear_fp8")
+    return out
+
+
+def linear_fp8_backward(dY: torch.Tensor, Xt, Wt, dtype=torch.float8_e4m3fn, dW: torch.Tensor | None = None,
+                        accumulate: bool = False, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """(dX, dW) of Y = X W^T: dX = dY W (of dY's type) and dW = dY^T X (float32; into
+    ``dW`` if given, added to it with ``accumulate``).  Xt and Wt are the operands
+    of the transposes, k rows of tokens and k rows of n values, as
+    quantize_fp8_pair makes them in the forward pass; dY (tokens x n) is
+    quantized to ``dtype`` in blocks of 1 x 128 along both its axes."""
+    scales = "float32" if Wt[1].dtype == torch.float32 else "pow2"
+    dy, dyt = quantize_fp8_pair(dY, (1, BLOCK), dtype, scales, stream=stream)
+    dX = gemm_fp8(dy, Wt, dtype=dY.dtype, stream=stream)
+    return dX, gemm_fp8(dyt, Xt, dtype=torch.float32, out=dW, accumulate=accumulate, stream=stream)
+
+
+def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                  out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The orthogonalised update of G (rows x cols, or a batch of such matrices;
+    float32, float16 or bfloat16): X = G / (||G|| + eps) in the Frobenius norm, then
+    ``steps`` times X <- a X + (b A + c A^2) X with A = X X^T on the shorter side.
+    ``coefficients``: (a, b, c), or one such triple for each step.  The result
+    (or ``out``) has G's shape and type."""
+    t = _type_of(G, "G")
+    if G.dim() not in (2, 3):
+        raise ValueError(f"G must be a matrix or a batch of matrices, got {G.dim()} dimensions")
+    _here(G, "G")
+    rows, cols = G.shape[-2:]
+    batch = G.size(0) if G.dim() == 3 else 1
+    og, ldg = _order(rows, cols, G.stride(-2), G.stride(-1), "G")
+    if out is None:
+        if og == b"R":
+            out = _empty(tuple(G.shape), G.dtype, G.device, stream)
+        else:
+            out = _empty(tuple(G.shape[:-2]) + (cols, rows), G.dtype, G.device, stream).transpose(-2, -1)
+    elif out.shape != G.shape or out.dtype != G.dtype:
+        raise ValueError(f"out must be {G.dtype} of shape {tuple(G.shape)}")
+    _here(out, "out")
+    oo, ldo = _order(rows, cols, out.stride(-2), out.stride(-1), "out")
+    flat = [float(c) for k in coefficients for c in (k if hasattr(k, "__len__") else (k,))]
+    if len(flat) == 3:
+        flat = flat * max(steps, 0)
+    if steps >= 0 and len(flat) != 3 * steps:
+        raise ValueError(f"coefficients must be one triple or {steps} of them")
+    coef = (ctypes.c_double * max(len(flat), 1))(*flat)
+    ws, at, nbytes = _scratch(_L.o2m_orthogonalize_workspace(batch, rows, cols, t), out.device, stream)
+    _check(_L.o2m_orthogonalize(batch, rows, cols, G.data_ptr(), og, ldg, G.stride(0) if G.dim() == 3 else 0,
+                                out.data_ptr(), oo, ldo, out.stride(0) if G.dim() == 3 else 0, t, steps,
+                                ctypes.addressof(coef), eps, at, nbytes, _stream(stream)), "orthogonalize")
+    return out
