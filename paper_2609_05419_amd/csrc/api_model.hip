@@ -103,11 +103,10 @@ o2m_status o2m_gemm_fp8(int m, int n, int k, const o2m_fp8_operand *A, const o2m
     if (ldc < (order == 'R' ? n : m) || ldc < 1) return -9;
     if (!any) return O2M_OK;
     const hipStream_t st = (hipStream_t)stream;
-    // the kernels write the first operand's rows contiguously
-    const bool swap = order == 'R';
+    const bool swap = order == 'C';
     if (k == 0) {
         if (accumulate) return O2M_OK;
-        return hip_fail(launch_zero_out(C, swap ? n : m, swap ? m : n, ldc, type_bytes(c_type), st));
+        return hip_fail(launch_zero_out(C, swap ? m : n, swap ? n : m, ldc, type_bytes(c_type), st));
     }
     if (A->ld >= kMaxPitch || B->ld >= kMaxPitch) return O2M_ERR_SIZE;
     const o2m_status s = check_workspace(gemm_fp8_workspace(m, n, k), workspace, workspace_bytes);
@@ -143,7 +142,7 @@ o2m_status o2m_linear_fp8(int tokens, int n, int k, const void *X, int x_type, i
     const o2m_fp8_operand q = kept_x(tokens, k, W->scale_type, workspace);
     const hipError_t e = launch_quantize(tokens, k, X, x_type, ldx, &q, nullptr, st);
     if (e != hipSuccess) return hip_fail(e);
-    return hip_fail(launch_gemm_fp8(n, tokens, k, *W, q, Y, x_type, ldy, false,
+    return hip_fail(launch_gemm_fp8(tokens, n, k, q, *W, Y, x_type, ldy, false,
                                     static_cast<char *>(workspace) + kept_x_bytes(tokens, k), st));
 }
 

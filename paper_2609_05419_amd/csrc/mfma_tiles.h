@@ -15,6 +15,7 @@
 
 namespace o2m {
 
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_ptr;
@@ -72,9 +73,9 @@ __device__ inline void clear_row_tail(uint8_t *stage, int row, int left) {
 __device__ inline v8i read_fragment(const uint8_t *stage, int row0, int lane) {
     const int row = row0 + (lane & 15), c = 2 * (lane >> 4);
     const uint8_t *p = stage + row * kStageRowBytes;
-    const int4 lo = *reinterpret_cast<const int4 *>(p + ((c ^ (row & 7)) << 4));
-    const int4 hi = *reinterpret_cast<const int4 *>(p + (((c + 1) ^ (row & 7)) << 4));
-    return v8i{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    const v4i lo = *reinterpret_cast<const v4i *>(p + ((c ^ (row & 7)) << 4));
+    const v4i hi = *reinterpret_cast<const v4i *>(p + (((c + 1) ^ (row & 7)) << 4));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 }  // namespace o2m

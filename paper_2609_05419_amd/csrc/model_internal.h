@@ -23,7 +23,7 @@ inline int64_t round_up64(int64_t x, int64_t q) { return ceil_div(x, q) * q; }
 hipError_t launch_quantize(int lines, int len, const void *X, int type, int64_t ld, const o2m_fp8_operand *along,
                            const o2m_fp8_operand *across, hipStream_t st);
 
-// C = A B^T with C's m contiguous: entry (i, j) at C[i + j ldc].
+// C = A B^T, entry (i, j) at C[i ldc + j].
 hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const o2m_fp8_operand &B, void *C, int type,
                            int64_t ldc, bool accumulate, void *ws, hipStream_t st);
 size_t gemm_fp8_workspace(int m, int n, int k);

@@ -78,13 +78,14 @@ def product_bound(a, b, exact, dtype):
     the type.  16-bit results: the 8-bit matrix unit adds groups of 8 neighbouring
     products cut off 13 bits below the exponent of the largest, so each of the
     other 7 is off by less than 2^-13 of the power of two at or below the largest,
-    7 2^-13 < 2^-10 of the largest for the group."""
+    7 2^-13 < 2^-10 of the largest for the group, which is at most the product of
+    the largest factors."""
     k = a.shape[1]
     with np.errstate(invalid="ignore"):
         sums = (k + 4) * 2.0 ** -23 * (np.abs(a) @ np.abs(b).T)
         if dtype != torch.float32:
-            for g in range(0, k, 8):
-                sums += 2.0 ** -10 * (np.abs(a[:, None, g:g + 8]) * np.abs(b[None, :, g:g + 8])).max(-1)
+            top = lambda x: np.pad(np.abs(x), ((0, 0), (0, -k % 8))).reshape(len(x), -1, 8).max(-1)  # noqa: E731
+            sums += 2.0 ** -10 * (top(a) @ top(b).T)
     tiny = {torch.float32: 2.0 ** -150, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}[dtype]
     return sums + half_step(dtype) * (np.abs(exact) + sums) + tiny
 

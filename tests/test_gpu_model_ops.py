@@ -137,6 +137,31 @@ def test_gemm(o2m, m, n, k, scales):
         assert torch.equal(C, o2m.gemm_fp8(A, B, dtype=dtype))
 
 
+@pytest.mark.parametrize("m,n,k", [(1290, 1601, 128), (1290, 1601, 97), (1537, 1283, 300), (1536, 2048, 256), (1400, 1900, 1041),
+                                   (8, 8200, 700), (9000, 130, 2064)])
+@pytest.mark.parametrize("scales", ["pow2", "float32"])
+def test_gemm_large(o2m, m, n, k, scales):
+    """Enough tiles of 256 x 256 for the kernels of large products: one stage and
+    many, odd and even numbers of them, ends of k within 16 bytes, ragged edges."""
+    for i, (ba, bb, fa, fb, dtype) in enumerate([(1, 128, E4M3, E4M3, torch.bfloat16), (1, 1, E5M2, E4M3, torch.float16),
+                                                 (128, 1, E4M3, E5M2, torch.bfloat16), (128, 128, E5M2, E5M2, torch.float32)]):
+        a, b = matrix(m, k, 20 + i, spread=0.5), matrix(n, k, 40 + i, spread=0.5)
+        a[m // 2, k // 3], b[n - 1, k - 1] = float("nan"), float("inf")
+        A = o2m.quantize_fp8(a, (ba, 128), fa, scales)
+        B = o2m.quantize_fp8(b, (bb, 128), fb, scales)
+        if i % 2:   # rows behind which NaN lies
+            A, _ = padded_operand(o2m, a, ba, fa, scales)
+            A = o2m.Fp8Operand(A.values, A.scales.t().contiguous().t())
+        print("gemm", m, n, k, scales, ba, bb, flush=True)
+        C = o2m.gemm_fp8(A, B, dtype=dtype)
+        R.check_product(C, R.values64(A, ba), R.values64(B, bb), dtype)
+        again = o2m.gemm_fp8(A, B, dtype=dtype)
+        assert torch.equal(C.view(torch.uint8), again.view(torch.uint8))   # NaN as well
+        out = torch.ones((n, m), dtype=dtype, device=DEV).t()
+        R.check_product(o2m.gemm_fp8(A, B, out=out, accumulate=True), R.values64(A, ba), R.values64(B, bb), dtype,
+                        np.ones((m, n)))
+
+
 @pytest.mark.parametrize("scales", ["pow2", "float32"])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_gemm_out(o2m, scales, dtype):
