@@ -113,14 +113,13 @@ __global__ __launch_bounds__(256) void fp8_tile(Fp8Args g) {
     const int i0 = ti * T, j0 = tj * T;
     const auto ra = rows_of(g.a.values + i0 * g.a.ld, min(T, g.a.rows - i0), g.a.ld, g.k);
     const auto rb = rows_of(g.b.values + j0 * g.b.ld, min(T, g.b.rows - j0), g.b.ld, g.k);
-    const CopyLane cl = copy_lane(lane);
     auto copy = [&](int kb) {
         uint8_t *buf = lds + (kb & 1) * kBuf;
         const int left = g.k - kb * kBlockK;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            copy_rows(ra, buf + (wave * 4 + q) * 1024, cl, wave * 4 + q, (int)g.a.ld, kb, left);
-            copy_rows(rb, buf + T * kStageRowBytes + (wave * 4 + q) * 1024, cl, wave * 4 + q, (int)g.b.ld, kb, left);
+            copy_rows<0>(ra, buf + (wave * 4 + q) * 1024, lane, wave * 4 + q, (int)g.a.ld, kb, left);
+            copy_rows<0>(rb, buf + T * kStageRowBytes + (wave * 4 + q) * 1024, lane, wave * 4 + q, (int)g.b.ld, kb, left);
         }
     };
     const int wi = (wave >> 1) * 64, wj = (wave & 1) * 64;
@@ -157,8 +156,8 @@ __global__ __launch_bounds__(256) void fp8_tile(Fp8Args g) {
         v8i fa[4], fb[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            fa[i] = read_fragment(buf, wi + 16 * i, lane);
-            fb[i] = read_fragment(buf + T * kStageRowBytes, wj + 16 * i, lane);
+            fa[i] = read_fragment<0>(buf, wi + 16 * i + (lane & 15), lane);
+            fb[i] = read_fragment<0>(buf + T * kStageRowBytes, wj + 16 * i + (lane & 15), lane);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -263,7 +262,8 @@ struct ScaledOp {
         // VALU results before an MFMA of the assembly below reads them
         asm volatile("s_nop 1" : "+v"(a.use[0]), "+v"(a.use[1]), "+v"(b.use[0]), "+v"(b.use[1]));
     }
-    template <int I, int J>
+    static constexpr int kParts = 1;
+    template <int I, int J, int P>
     __device__ __forceinline__ void mma(v4f &d, const v8i &x, const v8i &y) {
         mfma_scaled<FA, FB, I & 3, J & 3>(d, x, y, a.use[I >> 2], b.use[J >> 2]);
     }
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(256, 1) void fp8_pipe(Fp8Args g) {
     op.b.init(g.b, j0 + w.row_b + 8 * q);
     v4f acc[8][8];
     pipe_run(w, op, src, g.kblocks, acc);
-    pipe_results(w, acc, [&](int row, int col, const v8f &v) { store8(g, i0 + row, j0 + col, v); });
+    pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) { store8(g, i0 + row, j0 + col, v); });
 }
 
 template <class T>

@@ -116,8 +116,8 @@ __device__ inline void pipe_zero(v4f (&acc)[8][8]) {
 // operands of a stage: a(s), b(s) descriptors, k(s) the stage within them, left(s)
 // the bytes from there on (<= 0 for s >= stages), ld_a, ld_b; Op the arithmetic:
 // fetch(s) asks for what stage s needs besides (it may issue any number of
-// loads), begin(s) takes it into use, mma<i, j>(acc[i][j], a, b) multiplies, and
-// mask(f, s) clears what the last stage's fragments hold past the rows' ends.
+// loads), begin(s) takes it into use, mma<i, j, p>(acc[i][j], a, b) multiplies, in
+// kParts MFMAs of 8 blocks' distance to each other, and mask(f, s) clears what the last stage's fragments hold past the rows' ends.
 //
 // Waits.  The copies of a wave are issued in the order .. A1(s) B(s+1) | A0(s+1) |
 // A1(s+1) B(s+2) | A0(s+2) .. (A0, A1: 4 copies of a half, B: 8), a bar being a
@@ -126,6 +126,7 @@ __device__ inline void pipe_zero(v4f (&acc)[8][8]) {
 // fetch() in between only make a wait stricter.
 template <class Op, class Src>
 __device__ inline void pipe_run(const PipeWave &w, Op &op, const Src &src, int stages, v4f (&acc)[8][8]) {
+    constexpr int P = Op::kParts;
     auto buffer = [&](int s) { return w.lds + (s & 1) * kPipeStage; };
     auto copy_a = [&](int s, int h, int t) {
         pipe_copy(w, src.a(s), src.ld_a, src.k(s), src.left(s), buffer(s), h, t);
@@ -159,22 +160,30 @@ __device__ inline void pipe_run(const PipeWave &w, Op &op, const Src &src, int s
         lds_barrier();
         op.begin(s);
         op.fetch(s + 1);
-        each<32>([&](auto T) {
-            constexpr int t = T, i = t >> 3, j = (i & 1) ? 7 - (t & 7) : t & 7, c = t >> 1;
-            if constexpr ((t & 7) == 0) a[(i + 1) & 1] = pipe_fragment(cur, w.frag_a, i + 1);
-            op.template mma<i, j>(acc[i][j], a[i & 1], bc[j]);
-            if constexpr ((t & 1) && c < 4) copy_a(s + 1, 1, c);
-            if constexpr ((t & 1) && c >= 4 && c < 12) copy_b(s + 2, c - 4);
+        // the 32 blocks of i = 0..3, kParts MFMAs each; m counts blocks' worth of
+        // MFMAs, after which the memory instructions follow
+        each<32 * P>([&](auto T) {
+            constexpr int t = T, i = t / (8 * P), p = t / 8 % P, j = (i & 1) ? 7 - (t & 7) : t & 7;
+            constexpr int m = t / P, c = m >> 1;
+            if constexpr (t % (8 * P) == 0) a[(i + 1) & 1] = pipe_fragment(cur, w.frag_a, i + 1);
+            op.template mma<i, j, p>(acc[i][j], a[i & 1], bc[j]);
+            if constexpr (t % P == P - 1) {
+                if constexpr ((m & 1) && c < 4) copy_a(s + 1, 1, c);
+                if constexpr ((m & 1) && c >= 4 && c < 12) copy_b(s + 2, c - 4);
+            }
         });
         wait_vmem<12>();
         lds_barrier();
-        each<32>([&](auto T) {
-            constexpr int t = T, i = 4 + (t >> 3), j = (i & 1) ? 7 - (t & 7) : t & 7;
-            if constexpr ((t & 7) == 0)
+        each<32 * P>([&](auto T) {
+            constexpr int t = T, i = 4 + t / (8 * P), p = t / 8 % P, j = (i & 1) ? 7 - (t & 7) : t & 7;
+            constexpr int m = t / P;
+            if constexpr (t % (8 * P) == 0)
                 a[(i + 1) & 1] = i < 7 ? pipe_fragment(cur, w.frag_a, i + 1) : pipe_fragment(next, w.frag_a, 0);
-            op.template mma<i, j>(acc[i][j], a[i & 1], bc[j]);
-            if constexpr ((t & 3) == 1) bn[t >> 2] = pipe_fragment(next, w.frag_b, t >> 2);
-            if constexpr ((t & 7) == 3) copy_a(s + 2, 0, t >> 3);
+            op.template mma<i, j, p>(acc[i][j], a[i & 1], bc[j]);
+            if constexpr (t % P == P - 1) {
+                if constexpr ((m & 3) == 1) bn[m >> 2] = pipe_fragment(next, w.frag_b, m >> 2);
+                if constexpr ((m & 7) == 3) copy_a(s + 2, 0, m >> 3);
+            }
         });
     };
     int s = 0;
@@ -199,9 +208,9 @@ __device__ inline void pipe_run(const PipeWave &w, Op &op, const Src &src, int s
         constexpr int i = I;
         if constexpr (i < 7) a[(i + 1) & 1] = pipe_fragment(cur, w.frag_a, i + 1);
         op.mask(a[i & 1], s);
-        each<8>([&](auto J) {
-            constexpr int j = J;
-            op.template mma<i, j>(acc[i][j], a[i & 1], b0[j]);
+        each<8 * P>([&](auto J) {
+            constexpr int j = J & 7;
+            op.template mma<i, j, J / 8>(acc[i][j], a[i & 1], b0[j]);
         });
     });
     wait_vmem<0>();
@@ -209,28 +218,33 @@ __device__ inline void pipe_run(const PipeWave &w, Op &op, const Src &src, int s
 }
 
 // out(row, col, v): 8 neighbouring outputs of a row of the wave's 128 x 128, for
-// all of them.  The accumulators go to LDS straight from their registers and
-// each lane reads its own back, 8 columns of 4 rows at a time: read as values
-// from a program they would all be copied at once, into scratch memory.  (The
-// round trip is some 2% of a tile of 64 stages.)
-template <class Out>
+// all of them; or, ACROSS, 8 neighbouring ones of a column, from `row` on.  The
+// accumulators go to LDS straight from their registers and each lane reads its
+// own back, 8 x 4 outputs at a time: read as values from a program they would
+// all be copied at once, into scratch memory.  (The round trip is some 2% of a
+// tile of 64 stages.)
+template <bool ACROSS, class Out>
 __device__ inline void pipe_results(const PipeWave &w, const v4f (&acc)[8][8], Out out) {
     uint8_t *mine = w.lds + w.wave * (kPipeLds / 4) + w.lane * 16;
     lds_barrier();   // every wave is done with the stages
     each<2>([&](auto H) {
         each<4>([&](auto I) {
-            each<8>([&](auto J) { *reinterpret_cast<v4f *>(mine + (I * 8 + J) * 1024) = acc[4 * H + I][J]; });
+            each<8>([&](auto J) {
+                *reinterpret_cast<v4f *>(mine + (I * 8 + J) * 1024) = ACROSS ? acc[J][4 * H + I] : acc[4 * H + I][J];
+            });
         });
-        const int row0 = w.row_a + 32 * (w.lane >> 4) + 4 * H, col = w.row_b + 8 * (w.lane & 15);
+        const int row0 = w.row_a + 32 * (w.lane >> 4), col0 = w.row_b + 8 * (w.lane & 15);
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {
             v4f u[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) u[j] = *reinterpret_cast<const v4f *>(mine + (i * 8 + j) * 1024);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                out(row0 + 8 * e + i, col,
-                    v8f{u[0][e], u[1][e], u[2][e], u[3][e], u[4][e], u[5][e], u[6][e], u[7][e]});
+            for (int e = 0; e < 4; ++e) {
+                const v8f v = {u[0][e], u[1][e], u[2][e], u[3][e], u[4][e], u[5][e], u[6][e], u[7][e]};
+                if (ACROSS) out(row0 + 8 * e, col0 + 4 * H + i, v);
+                else out(row0 + 8 * e + 4 * H + i, col0, v);
+            }
         }
     });
 }

@@ -4,9 +4,9 @@
 //
 // A stage of R rows is R x 128 bytes of LDS, row after row.  It arrives by
 // direct buffer->LDS copies of 1 KB per wave: 8 rows, each a whole 128-byte
-// line of its operand.  The 16-byte chunk c of row r lies in slot c ^ (r & 7)
+// line of its operand.  The 16-byte chunk c of row r lies in slot c ^ (r >> S & 7)
 // of its row, so that the lanes of a fragment read, which take one chunk of 16
-// different rows, spread over all banks.  The swizzle costs nothing: a copy's
+// rows 2^S apart, spread over all banks.  The swizzle costs nothing: a copy's
 // destination is fixed (lane x 16), its source address is each lane's own.
 #pragma once
 
@@ -46,19 +46,14 @@ __device__ inline __amdgpu_buffer_rsrc_t rows_of(const uint8_t *base, int rows, 
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), (short)0, extent, 0x00020000);
 }
 
-// One lane's part of a copy: its row (of 8) and the chunk that its slot holds.
-struct CopyLane {
-    int row, chunk16;   // chunk16: byte offset of the chunk within the stage row
-};
-__device__ inline CopyLane copy_lane(int lane) {
-    return {lane >> 3, ((lane & 7) ^ (lane >> 3)) * 16};
-}
-
 // Copy rows [8 q, 8 q + 8) of stage kb to dst (wave-uniform, 1 KB).  `left` is
-// the operand's bytes from this stage on: chunks past it are read as zeros.
-__device__ inline void copy_rows(__amdgpu_buffer_rsrc_t r, uint8_t *dst, CopyLane c, int q, int ld, int kb, int left) {
-    int off = (8 * q + c.row) * ld + c.chunk16;
-    if (left < kStageRowBytes) off = c.chunk16 < left ? off : 0x7FFFFFF0;
+// the operand's bytes from this stage on: chunks past it are read as zeros.  S:
+// the chunk c of row r lies in slot c ^ (r >> S & 7).
+template <int S>
+__device__ inline void copy_rows(__amdgpu_buffer_rsrc_t r, uint8_t *dst, int lane, int q, int ld, int kb, int left) {
+    const int row = 8 * q + (lane >> 3), chunk16 = ((lane & 7) ^ (row >> S & 7)) << 4;
+    int off = row * ld + chunk16;
+    if (left < kStageRowBytes) off = chunk16 < left ? off : 0x7FFFFFF0;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr *)dst, 16, off, kb * kStageRowBytes, 0, 0);
 }
 
@@ -68,13 +63,14 @@ __device__ inline void clear_row_tail(uint8_t *stage, int row, int left) {
     for (int b = left & 15; b < 16; ++b) chunk[b] = 0;
 }
 
-// The 32 bytes of a fragment that one lane holds: row lane % 16 of the 16, bytes
-// [32 g, 32 g + 32) of the stage row with g = lane / 16.
-__device__ inline v8i read_fragment(const uint8_t *stage, int row0, int lane) {
-    const int row = row0 + (lane & 15), c = 2 * (lane >> 4);
+// The 32 bytes of a fragment that one lane holds: of `row`, bytes [32 g, 32 g +
+// 32) of the stage row with g = lane / 16.
+template <int S>
+__device__ inline v8i read_fragment(const uint8_t *stage, int row, int lane) {
+    const int slot = (2 * (lane >> 4)) ^ (row >> S & 7);
     const uint8_t *p = stage + row * kStageRowBytes;
-    const v4i lo = *reinterpret_cast<const v4i *>(p + ((c ^ (row & 7)) << 4));
-    const v4i hi = *reinterpret_cast<const v4i *>(p + (((c + 1) ^ (row & 7)) << 4));
+    const v4i lo = *reinterpret_cast<const v4i *>(p + (slot << 4));
+    const v4i hi = *reinterpret_cast<const v4i *>(p + ((slot ^ 1) << 4));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 

@@ -308,6 +308,24 @@ def test_orthogonalize(o2m, rows, cols, dtype, order):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,rows,cols,order", [(1, 1100, 3900, "row"), (1, 2300, 1400, "col"), (40, 260, 300, "row")])
+def test_orthogonalize_large(o2m, batch, rows, cols, order, dtype):
+    """Enough tiles for the kernels of large products, the last ones beside the
+    matrix; a step or two, which the bound tells apart from anything else."""
+    g = torch.stack([matrix(rows, cols, 50 + i % 3, torch.float32, order, spread=0.3) for i in range(batch)]).to(dtype)
+    if order == "col":
+        g = g.transpose(1, 2).contiguous().transpose(1, 2)
+    print("orthogonalize", batch, rows, cols, dtype, order, flush=True)
+    x = o2m.orthogonalize(g, steps=2)
+    assert x.stride() == g.stride()
+    for i in (0, batch - 1):
+        check_orthogonalize(x[i], g[i], dtype, 2)
+    assert torch.equal(x, o2m.orthogonalize(g, steps=2))
+    turned = o2m.orthogonalize(g, steps=2, out=torch.empty_like(g.transpose(1, 2).contiguous()).transpose(1, 2))
+    assert torch.equal(x, turned)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_orthogonalize_batch_views_and_orders(o2m, dtype):
     """A batch, in rows at a distance, into outputs of the other order, behind
     which nothing changes; and in place."""
