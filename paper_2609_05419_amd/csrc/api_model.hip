@@ -116,7 +116,7 @@ o2m_status o2m_gemm_fp8(int m, int n, int k, const o2m_fp8_operand *A, const o2m
 }
 
 size_t o2m_linear_fp8_workspace(int tokens, int n, int k) {
-    if (tokens <= 0 || n <= 0 || k <= 0) return 0;
+    if (tokens <= 0 || n <= 0 || k <= 0 || linear_is_fused(tokens, k)) return 0;
     return kept_x_bytes(tokens, k) + gemm_fp8_workspace(tokens, n, k);
 }
 
@@ -139,6 +139,7 @@ o2m_status o2m_linear_fp8(int tokens, int n, int k, const void *X, int x_type, i
     if (W->ld >= kMaxPitch || round_up64(k, 16) >= kMaxPitch) return O2M_ERR_SIZE;
     const o2m_status s = check_workspace(o2m_linear_fp8_workspace(tokens, n, k), workspace, workspace_bytes);
     if (s != O2M_OK) return s;
+    if (linear_is_fused(tokens, k)) return hip_fail(launch_linear_fused(tokens, n, k, X, x_type, ldx, *W, Y, ldy, st));
     const o2m_fp8_operand q = kept_x(tokens, k, W->scale_type, workspace);
     const hipError_t e = launch_quantize(tokens, k, X, x_type, ldx, &q, nullptr, st);
     if (e != hipSuccess) return hip_fail(e);

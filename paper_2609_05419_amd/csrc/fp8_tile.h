@@ -1,0 +1,240 @@
+// Tiles of 8-bit block-scaled products whose partial sums are scaled by the vector
+// unit, and small ones of every kind; k_fp8.hip says which product takes what.
+#pragma once
+
+#include "fp8_operand.h"
+#include "mfma_pipe.h"
+#include "tile_schedule.h"
+
+namespace o2m {
+
+// How a block's products are added up.
+enum Sum {
+    kScaled,    // 8-bit MFMA with power-of-two scales
+    kPartial,   // 8-bit MFMA, then fp32 scales
+    kWide,      // fp16 MFMA, then scales of either kind
+};
+
+// C = A B^T, entry (i, j) at C[i ldc + j].
+struct Fp8Args {
+    Side a, b;
+    int k, kblocks;
+    int mt, nt, chunk;   // tiles; per XCD
+    void *C;
+    int64_t ldc;
+    int type, accumulate, vec;   // vec: rows of C allow 16-byte accesses
+    float *parts;        // split launches: sums [split][m][pitch]
+    int pitch, splits, per;
+};
+
+typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
+
+// Eight neighbouring outputs of a row, from `col` on: in 16-byte stores where
+// all exist and the rows allow it.
+__device__ inline void store8(const Fp8Args &g, int row, int col, v8f v) {
+    const int n = g.b.rows - col;
+    if (row >= g.a.rows || n <= 0) return;
+    const int64_t at = row * g.ldc + col;
+    if (g.vec && n >= 8) {
+        uint16_t *p = static_cast<uint16_t *>(g.C) + at;
+        if (g.type == O2M_TYPE_BF16) {
+            if (g.accumulate) v += __builtin_convertvector(*reinterpret_cast<const v8bf16 *>(p), v8f);
+            *reinterpret_cast<v8bf16 *>(p) = __builtin_convertvector(v, v8bf16);
+        } else if (g.type == O2M_TYPE_F16) {
+            if (g.accumulate) v += __builtin_convertvector(*reinterpret_cast<const v8f16 *>(p), v8f);
+            *reinterpret_cast<v8f16 *>(p) = __builtin_convertvector(v, v8f16);
+        } else {
+            v8f *q = reinterpret_cast<v8f *>(static_cast<float *>(g.C) + at);
+            if (g.accumulate) v += *q;
+            *q = v;
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < n) store_out(g.C, at + j, g.type, v[j] + (g.accumulate ? load_out(g.C, at + j, g.type) : 0.0f));
+}
+
+// Four neighbouring outputs of a row.
+__device__ inline void store4(const Fp8Args &g, int row, int col, v4f v) {
+    typedef _Float16 v4f16 __attribute__((ext_vector_type(4)));
+    typedef __bf16 v4bf16 __attribute__((ext_vector_type(4)));
+    const int n = g.b.rows - col;
+    if (row >= g.a.rows || n <= 0) return;
+    const int64_t at = row * g.ldc + col;
+    if (g.vec && n >= 4) {
+        uint16_t *p = static_cast<uint16_t *>(g.C) + at;
+        if (g.type == O2M_TYPE_BF16) {
+            if (g.accumulate) v += __builtin_convertvector(*reinterpret_cast<const v4bf16 *>(p), v4f);
+            *reinterpret_cast<v4bf16 *>(p) = __builtin_convertvector(v, v4bf16);
+        } else if (g.type == O2M_TYPE_F16) {
+            if (g.accumulate) v += __builtin_convertvector(*reinterpret_cast<const v4f16 *>(p), v4f);
+            *reinterpret_cast<v4f16 *>(p) = __builtin_convertvector(v, v4f16);
+        } else {
+            v4f *q = reinterpret_cast<v4f *>(static_cast<float *>(g.C) + at);
+            if (g.accumulate) v += *q;
+            *q = v;
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < n) store_out(g.C, at + j, g.type, v[j] + (g.accumulate ? load_out(g.C, at + j, g.type) : 0.0f));
+}
+
+// WR x WC waves of M x 4 blocks of 16 x 16; two stage buffers.  Rows of a wave are
+// 16 i + q (block i, q = lane % 16), columns 4 q + j, so that a lane's blocks j are
+// neighbouring columns.  Each thread fetches the scale of one row of A or B a stage
+// ahead and passes it on in LDS.  WB: B's scale is one for the wave's columns.
+template <int WR, int WC, int M>
+struct TileOf {
+    static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
+    static constexpr int kTm = WR * M * 16, kTn = WC * 64;
+    static constexpr int kWaveCols = WC;
+    static constexpr int kBuf = (kTm + kTn) * kStageRowBytes;
+    static_assert(kTm + kTn == kThreads && kTm == 32 * kWaves && kTn == 32 * kWaves, "a row of A or B for each thread");
+};
+
+template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M>
+__global__ __launch_bounds__(64 * WR * WC, 2) void fp8_tile(Fp8Args g) {
+    typedef TileOf<WR, WC, M> T;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * T::kBuf + 2 * T::kThreads * 4];
+    uint32_t *const scales = reinterpret_cast<uint32_t *>(lds + 2 * T::kBuf);   // [2][A's rows, B's rows]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int z = blockIdx.x % g.splits, slot = blockIdx.x / g.splits;
+    const TileCoord tc = tile_of(slot & 7, slot >> 3, g.mt, g.nt, g.chunk, 0);
+    if (!tc.valid) return;   // whole workgroup
+    const int i0 = tc.ti * T::kTm, j0 = tc.tj * T::kTn;
+    const auto ra = rows_of(g.a.values + i0 * g.a.ld, min(T::kTm, g.a.rows - i0), g.a.ld, g.k);
+    const auto rb = rows_of(g.b.values + j0 * g.b.ld, min(T::kTn, g.b.rows - j0), g.b.ld, g.k);
+    const int s0 = z * g.per, s1 = min(g.kblocks, s0 + g.per);
+    auto copy = [&](int kb) {
+        uint8_t *buf = lds + (kb & 1) * T::kBuf;
+        const int left = g.k - kb * kBlockK;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            copy_rows<0>(ra, buf + (wave * 4 + q) * 1024, lane, wave * 4 + q, (int)g.a.ld, kb, left);
+            copy_rows<2>(rb, buf + T::kTm * kStageRowBytes + (wave * 4 + q) * 1024, lane, wave * 4 + q, (int)g.b.ld, kb, left);
+        }
+    };
+    const bool mine_a = tid < T::kTm;
+    const Side &side = mine_a ? g.a : g.b;
+    const int64_t scale_row = scale_index(side, mine_a ? i0 + tid : j0 + tid - T::kTm, 0);
+    auto fetch = [&](int kb) -> uint32_t {
+        const int64_t at = scale_row + kb * side.s_blk;
+        return side.pow2 ? static_cast<const uint8_t *>(side.scales)[at] : static_cast<const uint32_t *>(side.scales)[at];
+    };
+    const int wi = wave / WC * (M * 16), wj = wave % WC * 64, q = lane & 15;
+    v4f acc[M][4];
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+    uint32_t next = 0;
+    if (s0 < s1) {
+        next = fetch(s0);
+        copy(s0);
+    }
+    for (int kb = s0; kb < s1; ++kb) {
+        scales[(kb & 1) * T::kThreads + tid] =
+            SUM == kWide && side.pow2 ? __float_as_uint(code_value(next)) : next;
+        wait_vmem<0>();
+        lds_barrier();
+        uint8_t *buf = lds + (kb & 1) * T::kBuf;
+        const int left = g.k - kb * kBlockK;
+        if (left < kBlockK && (left & 15)) {   // uniform: the last stage of an odd k
+            clear_row_tail(buf, tid, left, mine_a ? 0 : 2);
+            lds_barrier();
+        }
+        if (kb + 1 < s1) {
+            next = fetch(kb + 1);
+            copy(kb + 1);
+        }
+        const uint32_t *sc = scales + (kb & 1) * T::kThreads;
+        const v4i cb = *reinterpret_cast<const v4i *>(sc + T::kTm + wj + 4 * q);   // codes, or floats' bits
+        const v4f sb = __builtin_bit_cast(v4f, cb);
+        v8i fb[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) fb[j] = read_fragment<2>(buf + T::kTm * kStageRowBytes, wj + 4 * q + j, lane);
+        v8f16 wb[SUM == kWide ? 4 : 1][4];
+        if constexpr (SUM == kWide) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) wb[j][h] = widen<FB>(fb[j][2 * h], fb[j][2 * h + 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const v8i fa = read_fragment<0>(buf, wi + 16 * i + q, lane);
+            if constexpr (SUM == kScaled) {
+                const int ca = (int)sc[wi + 16 * i + q];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                        fa, fb[j], acc[i][j], FA, FB, 0, ca, 0, cb[j]);
+            } else {
+                v4f sa = *reinterpret_cast<const v4f *>(sc + wi + 16 * i + 4 * (lane >> 4));
+                if (WB) sa *= sb[0];
+                v8f16 wa[4];
+                if constexpr (SUM == kWide) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) wa[h] = widen<FA>(fa[2 * h], fa[2 * h + 1]);
+                }
+                v4f p[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[j] = v4f{0, 0, 0, 0};
+                if constexpr (SUM == kPartial) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        p[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[j], p[j], FA, FB, 0, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            p[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wa[h], wb[j][h], p[j], 0, 0, 0);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[i][j][e] = fmaf(p[j][e], WB ? sa[e] : sa[e] * sb[j], acc[i][j][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = i0 + wi + 16 * i + 4 * (lane >> 4) + e, col = j0 + wj + 4 * q;
+            const v4f v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+            if (g.splits == 1) store4(g, row, col, v);
+            else if (row < g.a.rows && col < g.pitch)
+                *reinterpret_cast<v4f *>(g.parts + ((int64_t)z * g.a.rows + row) * g.pitch + col) = v;
+        }
+}
+
+template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M>
+hipError_t launch_tile(Fp8Args &g, hipStream_t st) {
+    typedef TileOf<WR, WC, M> T;
+    g.mt = (int)ceil_div(g.a.rows, T::kTm);
+    g.nt = (int)ceil_div(g.b.rows, T::kTn);
+    const int64_t chunk = ceil_div((int64_t)g.mt * g.nt, kXcds), grid = kXcds * chunk * g.splits;
+    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+    g.chunk = (int)chunk;
+    fp8_tile<SUM, FA, FB, WB, WR, WC, M><<<(unsigned)grid, T::kThreads, 0, st>>>(g);
+    return hipGetLastError();
+}
+
+// Tiles of 256 x 256 by 8 waves (large) or 128 x 128 by 4.
+template <Sum SUM, int FA, int FB, bool WB>
+hipError_t launch_sizes(Fp8Args &g, bool large, hipStream_t st) {
+    return large ? launch_tile<SUM, FA, FB, WB, 2, 4, 8>(g, st) : launch_tile<SUM, FA, FB, WB, 2, 2, 4>(g, st);
+}
+
+// One file each; format: of A x 2 + of B.
+hipError_t launch_fp8_scaled(Fp8Args &g, int format, bool pipe, hipStream_t st);
+hipError_t launch_fp8_partial(Fp8Args &g, int format, bool large, hipStream_t st);
+hipError_t launch_fp8_wide(Fp8Args &g, int format, bool large, hipStream_t st);
+
+}  // namespace o2m

@@ -58,8 +58,8 @@ __device__ inline void copy_rows(__amdgpu_buffer_rsrc_t r, uint8_t *dst, int lan
 }
 
 // Zero the bytes of row `row` past `left` in the chunk that holds byte `left`.
-__device__ inline void clear_row_tail(uint8_t *stage, int row, int left) {
-    uint8_t *chunk = stage + row * kStageRowBytes + (((left >> 4) ^ (row & 7)) << 4);
+__device__ inline void clear_row_tail(uint8_t *stage, int row, int left, int s) {
+    uint8_t *chunk = stage + row * kStageRowBytes + (((left >> 4) ^ (row >> s & 7)) << 4);
     for (int b = left & 15; b < 16; ++b) chunk[b] = 0;
 }
 

@@ -28,6 +28,15 @@ hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const 
                            int64_t ldc, bool accumulate, void *ws, hipStream_t st);
 size_t gemm_fp8_workspace(int m, int n, int k);
 
+// The same with few tokens, W the operand with the many rows; entry (t, r) of Y at
+// t y_tok + r y_row.
+hipError_t launch_few(int tokens, int n, int k, const o2m_fp8_operand &X, const o2m_fp8_operand &W, void *Y, int type,
+                      int64_t y_tok, int64_t y_row, bool accumulate, hipStream_t st);
+// The linear layer in one launch, where linear_is_fused.
+bool linear_is_fused(int tokens, int k);
+hipError_t launch_linear_fused(int tokens, int n, int k, const void *X, int x_type, int64_t ldx, const o2m_fp8_operand &W,
+                               void *Y, int64_t ldy, hipStream_t st);
+
 struct OrthoArgs {
     int batch, rows, cols;          // of the work matrix: rows <= cols
     const void *G;
