@@ -56,4 +56,23 @@ __device__ inline uint32_t pack_fp8(const float (&y)[4], int format) {
     return (uint32_t)r;
 }
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+// Eight entries of one line from `x0`, of which `n` exist; zeros after them.  (The
+// loads need no alignment but the entries' own.)
+template <class T>
+__device__ inline void load8(const T *x0, int n, float (&v)[8]) {
+    if (n >= 8) {
+        u32x4 w[sizeof(T) / 2];
+        __builtin_memcpy(w, x0, sizeof w);
+        T t[8];
+        __builtin_memcpy(t, w, sizeof w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = as_float(t[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? as_float(x0[j]) : 0.0f;
+    }
+}
+
 }  // namespace o2m

@@ -22,84 +22,79 @@ struct Fp8Args {
     int mt, nt, chunk;   // tiles; per XCD
     void *C;
     int64_t ldc;
-    int type, accumulate, vec;   // vec: rows of C allow 16-byte accesses
+    int type, accumulate;
     float *parts;        // split launches: sums [split][m][pitch]
     int pitch, splits, per;
 };
 
 typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
 
-// Eight neighbouring outputs of a row, from `col` on: in 16-byte stores where
-// all exist and the rows allow it.
-__device__ inline void store8(const Fp8Args &g, int row, int col, v8f v) {
+// N (4 or 8) neighbouring outputs of a row, from `col` on, at once where all exist.
+// (The accesses need no alignment but the entries' own.)
+template <int N, class V>
+__device__ inline void store_run(const Fp8Args &g, int row, int col, V v) {
+    typedef _Float16 vf16 __attribute__((ext_vector_type(N)));
+    typedef __bf16 vbf16 __attribute__((ext_vector_type(N)));
     const int n = g.b.rows - col;
     if (row >= g.a.rows || n <= 0) return;
     const int64_t at = row * g.ldc + col;
-    if (g.vec && n >= 8) {
-        uint16_t *p = static_cast<uint16_t *>(g.C) + at;
-        if (g.type == O2M_TYPE_BF16) {
-            if (g.accumulate) v += __builtin_convertvector(*reinterpret_cast<const v8bf16 *>(p), v8f);
-            *reinterpret_cast<v8bf16 *>(p) = __builtin_convertvector(v, v8bf16);
+    if (n >= N) {
+        if (g.type == O2M_TYPE_F32) {
+            float *p = static_cast<float *>(g.C) + at;
+            V old;
+            if (g.accumulate) {
+                __builtin_memcpy(&old, p, sizeof old);
+                v += old;
+            }
+            __builtin_memcpy(p, &v, sizeof v);
         } else if (g.type == O2M_TYPE_F16) {
-            if (g.accumulate) v += __builtin_convertvector(*reinterpret_cast<const v8f16 *>(p), v8f);
-            *reinterpret_cast<v8f16 *>(p) = __builtin_convertvector(v, v8f16);
+            _Float16 *p = static_cast<_Float16 *>(g.C) + at;
+            vf16 h;
+            if (g.accumulate) {
+                __builtin_memcpy(&h, p, sizeof h);
+                v += __builtin_convertvector(h, V);
+            }
+            h = __builtin_convertvector(v, vf16);
+            __builtin_memcpy(p, &h, sizeof h);
         } else {
-            v8f *q = reinterpret_cast<v8f *>(static_cast<float *>(g.C) + at);
-            if (g.accumulate) v += *q;
-            *q = v;
+            __bf16 *p = static_cast<__bf16 *>(g.C) + at;
+            vbf16 h;
+            if (g.accumulate) {
+                __builtin_memcpy(&h, p, sizeof h);
+                v += __builtin_convertvector(h, V);
+            }
+            h = __builtin_convertvector(v, vbf16);
+            __builtin_memcpy(p, &h, sizeof h);
         }
         return;
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < N; ++j)
         if (j < n) store_out(g.C, at + j, g.type, v[j] + (g.accumulate ? load_out(g.C, at + j, g.type) : 0.0f));
 }
 
-// Four neighbouring outputs of a row.
-__device__ inline void store4(const Fp8Args &g, int row, int col, v4f v) {
-    typedef _Float16 v4f16 __attribute__((ext_vector_type(4)));
-    typedef __bf16 v4bf16 __attribute__((ext_vector_type(4)));
-    const int n = g.b.rows - col;
-    if (row >= g.a.rows || n <= 0) return;
-    const int64_t at = row * g.ldc + col;
-    if (g.vec && n >= 4) {
-        uint16_t *p = static_cast<uint16_t *>(g.C) + at;
-        if (g.type == O2M_TYPE_BF16) {
-            if (g.accumulate) v += __builtin_convertvector(*reinterpret_cast<const v4bf16 *>(p), v4f);
-            *reinterpret_cast<v4bf16 *>(p) = __builtin_convertvector(v, v4bf16);
-        } else if (g.type == O2M_TYPE_F16) {
-            if (g.accumulate) v += __builtin_convertvector(*reinterpret_cast<const v4f16 *>(p), v4f);
-            *reinterpret_cast<v4f16 *>(p) = __builtin_convertvector(v, v4f16);
-        } else {
-            v4f *q = reinterpret_cast<v4f *>(static_cast<float *>(g.C) + at);
-            if (g.accumulate) v += *q;
-            *q = v;
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (j < n) store_out(g.C, at + j, g.type, v[j] + (g.accumulate ? load_out(g.C, at + j, g.type) : 0.0f));
-}
-
-// WR x WC waves of M x 4 blocks of 16 x 16; two stage buffers.  Rows of a wave are
-// 16 i + q (block i, q = lane % 16), columns 4 q + j, so that a lane's blocks j are
-// neighbouring columns.  Each thread fetches the scale of one row of A or B a stage
-// ahead and passes it on in LDS.  WB: B's scale is one for the wave's columns.
-template <int WR, int WC, int M>
+// WR x WC waves of M x 4 blocks of 16 x 16 and a ring of S stage buffers.  Rows of a
+// wave are 16 i + q (block i, q = lane % 16), columns 4 q + j, so that a lane's
+// blocks j are neighbouring columns.  WB: B's scale is one for the wave's columns.
+template <int WR, int WC, int M, int S>
 struct TileOf {
     static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
-    static constexpr int kTm = WR * M * 16, kTn = WC * 64;
-    static constexpr int kWaveCols = WC;
-    static constexpr int kBuf = (kTm + kTn) * kStageRowBytes;
-    static_assert(kTm + kTn == kThreads && kTm == 32 * kWaves && kTn == 32 * kWaves, "a row of A or B for each thread");
+    static constexpr int kTm = WR * M * 16, kTn = WC * 64, kRows = kTm + kTn;
+    static constexpr int kCopyA = kTm / 8 / kWaves, kCopyB = kTn / 8 / kWaves;
+    static constexpr int kBuf = kRows * kStageRowBytes;
+    static constexpr int kIssues = kCopyA + kCopyB + 1;   // vector-memory instructions of a stage: copies, a scale
+    static_assert(kRows <= kThreads && kCopyA * 8 * kWaves == kTm && kCopyB * 8 * kWaves == kTn, "shares of a stage");
+    static_assert((S - 2) * kIssues <= 63, "what a wait can count");
 };
 
-template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M>
-__global__ __launch_bounds__(64 * WR * WC, 2) void fp8_tile(Fp8Args g) {
-    typedef TileOf<WR, WC, M> T;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * T::kBuf + 2 * T::kThreads * 4];
-    uint32_t *const scales = reinterpret_cast<uint32_t *>(lds + 2 * T::kBuf);   // [2][A's rows, B's rows]
+// Stage kb lies in buffer (kb - s0) % S, and S - 1 stages ahead are on their way.
+// Each thread fetches the scale of one row of A or B as far ahead, into a
+// register, and passes it on in LDS when the stage begins.
+template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M, int S, int OCC>
+__global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
+    typedef TileOf<WR, WC, M, S> T;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S * T::kBuf + 2 * T::kRows * 4];
+    uint32_t *const scales = reinterpret_cast<uint32_t *>(lds + S * T::kBuf);   // [2][A's rows, B's rows]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int z = blockIdx.x % g.splits, slot = blockIdx.x / g.splits;
     const TileCoord tc = tile_of(slot & 7, slot >> 3, g.mt, g.nt, g.chunk, 0);
@@ -108,18 +103,24 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void fp8_tile(Fp8Args g) {
     const auto ra = rows_of(g.a.values + i0 * g.a.ld, min(T::kTm, g.a.rows - i0), g.a.ld, g.k);
     const auto rb = rows_of(g.b.values + j0 * g.b.ld, min(T::kTn, g.b.rows - j0), g.b.ld, g.k);
     const int s0 = z * g.per, s1 = min(g.kblocks, s0 + g.per);
-    auto copy = [&](int kb) {
-        uint8_t *buf = lds + (kb & 1) * T::kBuf;
+    auto copy = [&](int kb, uint8_t *buf) {
         const int left = g.k - kb * kBlockK;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            copy_rows<0>(ra, buf + (wave * 4 + q) * 1024, lane, wave * 4 + q, (int)g.a.ld, kb, left);
-            copy_rows<2>(rb, buf + T::kTm * kStageRowBytes + (wave * 4 + q) * 1024, lane, wave * 4 + q, (int)g.b.ld, kb, left);
+        for (int c = 0; c < T::kCopyA; ++c) {
+            const int q = wave * T::kCopyA + c;
+            copy_rows<0>(ra, buf + q * 1024, lane, q, (int)g.a.ld, kb, left);
+        }
+#pragma unroll
+        for (int c = 0; c < T::kCopyB; ++c) {
+            const int q = wave * T::kCopyB + c;
+            copy_rows<2>(rb, buf + T::kTm * kStageRowBytes + q * 1024, lane, q, (int)g.b.ld, kb, left);
         }
     };
-    const bool mine_a = tid < T::kTm;
+    // (threads past the rows fetch the last row's)
+    const int my_row = min(tid, T::kRows - 1);
+    const bool mine_a = my_row < T::kTm;
     const Side &side = mine_a ? g.a : g.b;
-    const int64_t scale_row = scale_index(side, mine_a ? i0 + tid : j0 + tid - T::kTm, 0);
+    const int64_t scale_row = scale_index(side, mine_a ? i0 + my_row : j0 + my_row - T::kTm, 0);
     auto fetch = [&](int kb) -> uint32_t {
         const int64_t at = scale_row + kb * side.s_blk;
         return side.pow2 ? static_cast<const uint8_t *>(side.scales)[at] : static_cast<const uint32_t *>(side.scales)[at];
@@ -130,27 +131,33 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void fp8_tile(Fp8Args g) {
     for (int i = 0; i < M; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = v4f{0, 0, 0, 0};
-    uint32_t next = 0;
-    if (s0 < s1) {
-        next = fetch(s0);
-        copy(s0);
-    }
-    for (int kb = s0; kb < s1; ++kb) {
-        scales[(kb & 1) * T::kThreads + tid] =
-            SUM == kWide && side.pow2 ? __float_as_uint(code_value(next)) : next;
-        wait_vmem<0>();
-        lds_barrier();
-        uint8_t *buf = lds + (kb & 1) * T::kBuf;
+    uint32_t ahead[S == 2 ? 1 : S];
+#pragma unroll
+    for (int u = 0; u < S - 1; ++u)
+        if (s0 + u < s1) {
+            ahead[u] = fetch(s0 + u);
+            copy(s0 + u, lds + u * T::kBuf);
+        }
+    // u = (kb - s0) % S; a: where its scale is; a constant for S > 2
+    auto stage = [&](int kb, int u, auto A) {
+        constexpr int a = A, a_next = S == 2 ? 0 : (a + S - 1) % S;
+        uint8_t *buf = lds + u * T::kBuf;
         const int left = g.k - kb * kBlockK;
+        if (tid < T::kRows)
+            scales[(kb & 1) * T::kRows + tid] = SUM == kWide && side.pow2 ? __float_as_uint(code_value(ahead[a])) : ahead[a];
+        // this stage has landed; those after it, if there are S - 2, need not
+        if (S > 2 && kb + S - 1 <= s1) wait_vmem<(S > 2 ? S - 2 : 0) * T::kIssues>();
+        else wait_vmem<0>();
+        lds_barrier();
         if (left < kBlockK && (left & 15)) {   // uniform: the last stage of an odd k
-            clear_row_tail(buf, tid, left, mine_a ? 0 : 2);
+            if (tid < T::kRows) clear_row_tail(buf, tid, left, mine_a ? 0 : 2);
             lds_barrier();
         }
-        if (kb + 1 < s1) {
-            next = fetch(kb + 1);
-            copy(kb + 1);
+        if (kb + S - 1 < s1) {
+            ahead[a_next] = fetch(kb + S - 1);
+            copy(kb + S - 1, lds + (u + S - 1) % S * T::kBuf);
         }
-        const uint32_t *sc = scales + (kb & 1) * T::kThreads;
+        const uint32_t *sc = scales + (kb & 1) * T::kRows;
         const v4i cb = *reinterpret_cast<const v4i *>(sc + T::kTm + wj + 4 * q);   // codes, or floats' bits
         const v4f sb = __builtin_bit_cast(v4f, cb);
         v8i fb[4];
@@ -201,6 +208,14 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void fp8_tile(Fp8Args g) {
                         acc[i][j][e] = fmaf(p[j][e], WB ? sa[e] : sa[e] * sb[j], acc[i][j][e]);
             }
         }
+    };
+    if constexpr (S == 2) {
+        for (int kb = s0; kb < s1; ++kb) stage(kb, (kb - s0) & 1, std::integral_constant<int, 0>());
+    } else {
+        for (int kb = s0; kb < s1; kb += S)
+            each<S>([&](auto U) {
+                if (kb + U < s1) stage(kb + U, U, U);
+            });
     }
 #pragma unroll
     for (int i = 0; i < M; ++i)
@@ -208,33 +223,42 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void fp8_tile(Fp8Args g) {
         for (int e = 0; e < 4; ++e) {
             const int row = i0 + wi + 16 * i + 4 * (lane >> 4) + e, col = j0 + wj + 4 * q;
             const v4f v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
-            if (g.splits == 1) store4(g, row, col, v);
+            if (g.splits == 1) store_run<4>(g, row, col, v);
             else if (row < g.a.rows && col < g.pitch)
                 *reinterpret_cast<v4f *>(g.parts + ((int64_t)z * g.a.rows + row) * g.pitch + col) = v;
         }
 }
 
-template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M>
+template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M, int S, int OCC>
 hipError_t launch_tile(Fp8Args &g, hipStream_t st) {
-    typedef TileOf<WR, WC, M> T;
+    typedef TileOf<WR, WC, M, S> T;
     g.mt = (int)ceil_div(g.a.rows, T::kTm);
     g.nt = (int)ceil_div(g.b.rows, T::kTn);
     const int64_t chunk = ceil_div((int64_t)g.mt * g.nt, kXcds), grid = kXcds * chunk * g.splits;
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
     g.chunk = (int)chunk;
-    fp8_tile<SUM, FA, FB, WB, WR, WC, M><<<(unsigned)grid, T::kThreads, 0, st>>>(g);
+    fp8_tile<SUM, FA, FB, WB, WR, WC, M, S, OCC><<<(unsigned)grid, T::kThreads, 0, st>>>(g);
     return hipGetLastError();
 }
 
-// Tiles of 256 x 256 by 8 waves (large) or 128 x 128 by 4.
+// Tile sizes: 256 x 256 by 8 waves (kPartial; kScaled has a kernel of its own), 128 x
+// 128 by 4 (two workgroups per CU), 64 x 64 by 4 (two, with twice the stages on
+// their way).
+enum TileSize { k256, k128, k64 };
 template <Sum SUM, int FA, int FB, bool WB>
-hipError_t launch_sizes(Fp8Args &g, bool large, hipStream_t st) {
-    return large ? launch_tile<SUM, FA, FB, WB, 2, 4, 8>(g, st) : launch_tile<SUM, FA, FB, WB, 2, 2, 4>(g, st);
+hipError_t launch_sizes(Fp8Args &g, TileSize size, hipStream_t st) {
+    switch (size) {
+    case k64: return launch_tile<SUM, FA, FB, WB, 4, 1, 1, 4, 2>(g, st);
+    case k128: return launch_tile<SUM, FA, FB, WB, 2, 2, 4, 2, 2>(g, st);
+    default: break;
+    }
+    if constexpr (SUM == kPartial) return launch_tile<SUM, FA, FB, WB, 2, 4, 8, 2, 2>(g, st);
+    return hipErrorInvalidValue;
 }
 
 // One file each; format: of A x 2 + of B.
-hipError_t launch_fp8_scaled(Fp8Args &g, int format, bool pipe, hipStream_t st);
-hipError_t launch_fp8_partial(Fp8Args &g, int format, bool large, hipStream_t st);
-hipError_t launch_fp8_wide(Fp8Args &g, int format, bool large, hipStream_t st);
+hipError_t launch_fp8_scaled(Fp8Args &g, int format, TileSize size, hipStream_t st);
+hipError_t launch_fp8_partial(Fp8Args &g, int format, TileSize size, hipStream_t st);
+hipError_t launch_fp8_wide(Fp8Args &g, int format, TileSize size, hipStream_t st);
 
 }  // namespace o2m

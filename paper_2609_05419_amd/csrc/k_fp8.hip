@@ -40,7 +40,7 @@ __global__ __launch_bounds__(256) void join_parts(Fp8Args g) {
         const float *p = g.parts + row * (int64_t)g.pitch + col;
         v4f v = *reinterpret_cast<const v4f *>(p);
         for (int z = 1; z < g.splits; ++z) v += *reinterpret_cast<const v4f *>(p + z * plane);
-        store4(g, row, col, v);
+        store_run<4>(g, row, col, v);
     }
 }
 
@@ -52,22 +52,33 @@ __global__ __launch_bounds__(256) void zero_out(T *C, int64_t m, int64_t total, 
 
 constexpr int kFewRows = 32;
 
+// The tiles of a launch, by how many there are.  Measured (us, power-of-two scales,
+// bf16; tiles of 256 x 256, 128 x 128, 64 x 64):
+//   4096 x 4096 x 4096   54    78   139      2048 x 2048 x 2048   28   19   23
+//   4096 x 4096 x 512    19    21    33      1000 x 1000 x 1000   21   11    7
+//   2048 x 4096 x 8192   79    77   132      512 x 2048 x 2048    27   17   10
+// (fp32 scales 4096^3 72, 86, 146.)  fp32 results take 128 x 128 for the largest too:
+// the widened fragments leave no registers for more (4096^3 145 us, with 256 x
+// 256 and registers spilled 151).  Tiles of 64 x 64 that leave CUs idle are split
+// along k until each has one, from 4 stages each: 300 x 300 x 8000 (25 tiles) 30 us
+// in one piece, 11.5 in 8; 64 x 4096 x 4096 (64) 16 and 10.7 in 4; 300 x 1283 x 2051
+// (105) 12.4 and 10.6 in 2; with 256 tiles the joining costs more than it brings
+// (1000^3 6.9 and 12.1).
 struct Plan {
-    bool few, large;
+    bool few;
+    TileSize size;
     int splits, per;
 };
-// Tiles of 256 x 256 from half a tile per CU on; below, tiles of 128 x 128, split
-// until two for each CU are in flight, from 4 stages each.
-Plan plan_fp8(int m, int n, int k) {
+Plan plan_fp8(int m, int n, int k, bool wide) {
     Plan p = {};
     const int kblocks = (int)ceil_div(k, kBlockK);
     p.splits = 1;
     p.per = kblocks;
     p.few = std::min(m, n) <= kFewRows;
-    p.large = ceil_div(m, 256) * ceil_div(n, 256) >= kCus / 2;
-    if (p.few || p.large) return p;
-    const int64_t tiles = ceil_div(m, 128) * ceil_div(n, 128);
-    const int64_t want = std::min<int64_t>(2 * kCus / std::min<int64_t>(tiles, 2 * kCus), std::max(1, kblocks / 4));
+    auto tiles = [&](int q) { return ceil_div(m, q) * ceil_div(n, q); };
+    p.size = tiles(256) >= 200 && !wide ? k256 : tiles(128) >= kCus ? k128 : k64;
+    if (p.few || p.size != k64) return p;
+    const int64_t want = std::min<int64_t>(kCus / std::min<int64_t>(tiles(64), kCus), std::max(1, kblocks / 4));
     p.per = (int)ceil_div(kblocks, want);
     p.splits = (int)ceil_div(kblocks, p.per);
     return p;
@@ -86,14 +97,14 @@ hipError_t launch_zero_out(void *C, int64_t m, int64_t n, int64_t ldc, int size,
 
 size_t gemm_fp8_workspace(int m, int n, int k) {
     // either order of the result: its rows are those of one operand or the other
-    const Plan p = plan_fp8(m, n, k);
+    const Plan p = plan_fp8(m, n, k, false);   // (the same splits for every type)
     if (p.splits == 1) return 0;
     return sizeof(float) * (size_t)p.splits * (size_t)std::max(m * round_up64(n, 4), n * round_up64(m, 4));
 }
 
 hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const o2m_fp8_operand &B, void *C, int type,
                            int64_t ldc, bool accumulate, void *ws, hipStream_t st) {
-    const Plan p = plan_fp8(m, n, k);
+    const Plan p = plan_fp8(m, n, k, type == O2M_TYPE_F32);
     if (p.few)
         return n <= m ? launch_few(n, m, k, B, A, C, type, 1, ldc, accumulate, st)
                       : launch_few(m, n, k, A, B, C, type, ldc, 1, accumulate, st);
@@ -106,7 +117,6 @@ hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const 
     g.ldc = ldc;
     g.type = type;
     g.accumulate = accumulate;
-    g.vec = reinterpret_cast<uintptr_t>(C) % 16 == 0 && ldc * (type == O2M_TYPE_F32 ? 4 : 2) % 16 == 0;
     g.parts = static_cast<float *>(ws);
     g.pitch = (int)round_up64(n, 4);
     g.splits = p.splits;
@@ -114,9 +124,10 @@ hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const 
     const int format = A.format * 2 + B.format;
     // the large kernel of power-of-two scales reads those of 8 rows at once
     auto fits = [](const Side &s) { return !s.by_row || (s.s_row == 1 && s.rows >= 8); };
-    const hipError_t e = type == O2M_TYPE_F32 ? launch_fp8_wide(g, format, p.large, st)
-                         : g.a.pow2           ? launch_fp8_scaled(g, format, p.large && fits(g.a) && fits(g.b), st)
-                                              : launch_fp8_partial(g, format, p.large, st);
+    const TileSize size = p.size == k256 && g.a.pow2 && !(fits(g.a) && fits(g.b)) ? k128 : p.size;
+    const hipError_t e = type == O2M_TYPE_F32 ? launch_fp8_wide(g, format, size, st)
+                         : g.a.pow2           ? launch_fp8_scaled(g, format, size, st)
+                                              : launch_fp8_partial(g, format, size, st);
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t threads = (int64_t)m * (g.pitch / 4);
     join_parts<<<(unsigned)std::min<int64_t>(ceil_div(threads, 256), 2048), 256, 0, st>>>(g);

@@ -19,7 +19,7 @@ namespace o2m {
 namespace {
 
 constexpr int kAhead = 4;          // blocks of W in flight per wave
-constexpr int kFusedBytes = 32768;   // quantized tokens kept in LDS
+constexpr int kFusedBytes = 16384;   // quantized tokens kept in LDS
 
 struct FewArgs {
     Side w, x;          // x.rows: tokens
@@ -79,8 +79,12 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows(FewArgs g) {
     uint8_t *join = lds + (FUSED ? kFusedBytes + 2048 : 0);
 
     Part w[kAhead];
-    auto fetch = [&](int kb) {
-        const int at = kb * kBlockK + 16 * quad;
+    // the n-th block that this workgroup takes: each begins elsewhere, so that the
+    // rows, often a power of two apart, are not all read at one offset at a time
+    const int turn = (int)(blockIdx.x % (unsigned)g.kblocks);
+    auto turned = [&](int n) { return n + turn < g.kblocks ? n + turn : n + turn - g.kblocks; };
+    auto fetch = [&](int n) {
+        const int at = n < g.kblocks ? turned(n) * kBlockK + 16 * quad : g.k;
         return Part{chunk(rw, w_off, at, g.k), chunk(rw, w_off, at + 64, g.k)};
     };
 #pragma unroll
@@ -93,8 +97,9 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows(FewArgs g) {
             const int t = b / g.kblocks, kb = b % g.kblocks, k0 = kb * kBlockK + 8 * q;
             float v[8], m = 0.0f;
             const int64_t at = t * g.ldx + k0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = k0 + j < g.k ? load_out(g.X, at + j, g.x_type) : 0.0f;
+            if (g.x_type == O2M_TYPE_F32) load8(static_cast<const float *>(g.X) + at, g.k - k0, v);
+            else if (g.x_type == O2M_TYPE_F16) load8(static_cast<const __half *>(g.X) + at, g.k - k0, v);
+            else load8(static_cast<const __hip_bfloat16 *>(g.X) + at, g.k - k0, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = fmaxf(m, magnitude(v[j]));
 #pragma unroll
@@ -150,14 +155,14 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows(FewArgs g) {
             for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(p[e], sw[e] * sx, acc[t][e]);
         }
     };
-    for (int kb = wave; kb < g.kblocks; kb += WAVES * kAhead) {
+    for (int n = wave; n < g.kblocks; n += WAVES * kAhead) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int at = kb + WAVES * i;
+            const int at = n + WAVES * i;
             if (at < g.kblocks) {   // uniform
                 Part now = w[i];
                 w[i] = fetch(at + WAVES * kAhead);
-                block(at, now);
+                block(turned(at), now);
             }
         }
     }
@@ -197,7 +202,7 @@ void launch_tokens(const FewArgs &g, hipStream_t st) {
 }  // namespace
 
 // Tokens for which a workgroup quantizes X itself.
-bool linear_is_fused(int tokens, int k) { return tokens <= 2 && tokens * round_up64(k, kBlockK) <= kFusedBytes; }
+bool linear_is_fused(int tokens, int k) { return tokens <= 16 && tokens * round_up64(k, kBlockK) <= kFusedBytes; }
 
 hipError_t launch_linear_fused(int tokens, int n, int k, const void *X, int x_type, int64_t ldx, const o2m_fp8_operand &W,
                                void *Y, int64_t ldy, hipStream_t st) {

@@ -7,16 +7,16 @@
 namespace o2m {
 
 template <int FA, int FB>
-static hipError_t launch(Fp8Args &g, bool large, hipStream_t st) {
-    return g.b.by_row ? launch_sizes<kPartial, FA, FB, false>(g, large, st) : launch_sizes<kPartial, FA, FB, true>(g, large, st);
+static hipError_t launch(Fp8Args &g, TileSize size, hipStream_t st) {
+    return g.b.by_row ? launch_sizes<kPartial, FA, FB, false>(g, size, st) : launch_sizes<kPartial, FA, FB, true>(g, size, st);
 }
 
-hipError_t launch_fp8_partial(Fp8Args &g, int format, bool large, hipStream_t st) {
+hipError_t launch_fp8_partial(Fp8Args &g, int format, TileSize size, hipStream_t st) {
     switch (format) {
-    case 0: return launch<0, 0>(g, large, st);
-    case 1: return launch<0, 1>(g, large, st);
-    case 2: return launch<1, 0>(g, large, st);
-    default: return launch<1, 1>(g, large, st);
+    case 0: return launch<0, 0>(g, size, st);
+    case 1: return launch<0, 1>(g, size, st);
+    case 2: return launch<1, 0>(g, size, st);
+    default: return launch<1, 1>(g, size, st);
     }
 }
 

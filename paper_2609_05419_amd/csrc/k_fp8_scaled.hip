@@ -1,7 +1,7 @@
 // 8-bit block-scaled products with power-of-two scales and 16-bit results: the
 // scaled MFMA applies them, so that nothing but MFMAs and the feeding of them is
 // left.  Large products take the pipeline of mfma_pipe.h (8192^3 400 us, 2.75
-// PFLOP/s), small ones tiles of 128 x 128.
+// PFLOP/s), small ones tiles of 128 x 128 and 64 x 64.
 #include "fp8_tile.h"
 
 namespace o2m {
@@ -116,12 +116,12 @@ __global__ __launch_bounds__(256, 1) void fp8_pipe(Fp8Args g) {
     op.b.init(g.b, j0 + w.row_b + 8 * q);
     v4f acc[8][8];
     pipe_run(w, op, src, g.kblocks, acc);
-    pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) { store8(g, i0 + row, j0 + col, v); });
+    pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) { store_run<8>(g, i0 + row, j0 + col, v); });
 }
 
 template <int FA, int FB>
-hipError_t launch(Fp8Args &g, bool pipe, hipStream_t st) {
-    if (!pipe) return launch_tile<kScaled, FA, FB, false, 2, 2, 4>(g, st);
+hipError_t launch(Fp8Args &g, TileSize size, hipStream_t st) {
+    if (size != k256) return launch_sizes<kScaled, FA, FB, false>(g, size, st);
     g.mt = (int)ceil_div(g.a.rows, kPipeTile);
     g.nt = (int)ceil_div(g.b.rows, kPipeTile);
     const int64_t chunk = ceil_div((int64_t)g.mt * g.nt, kXcds);
@@ -137,12 +137,12 @@ hipError_t launch(Fp8Args &g, bool pipe, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_fp8_scaled(Fp8Args &g, int format, bool pipe, hipStream_t st) {
+hipError_t launch_fp8_scaled(Fp8Args &g, int format, TileSize size, hipStream_t st) {
     switch (format) {
-    case 0: return launch<0, 0>(g, pipe, st);
-    case 1: return launch<0, 1>(g, pipe, st);
-    case 2: return launch<1, 0>(g, pipe, st);
-    default: return launch<1, 1>(g, pipe, st);
+    case 0: return launch<0, 0>(g, size, st);
+    case 1: return launch<0, 1>(g, size, st);
+    case 2: return launch<1, 0>(g, size, st);
+    default: return launch<1, 1>(g, size, st);
     }
 }
 

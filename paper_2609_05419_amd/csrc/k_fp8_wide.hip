@@ -6,12 +6,12 @@
 
 namespace o2m {
 
-hipError_t launch_fp8_wide(Fp8Args &g, int format, bool large, hipStream_t st) {
+hipError_t launch_fp8_wide(Fp8Args &g, int format, TileSize size, hipStream_t st) {
     switch (format) {
-    case 0: return launch_sizes<kWide, 0, 0, false>(g, large, st);
-    case 1: return launch_sizes<kWide, 0, 1, false>(g, large, st);
-    case 2: return launch_sizes<kWide, 1, 0, false>(g, large, st);
-    default: return launch_sizes<kWide, 1, 1, false>(g, large, st);
+    case 0: return launch_sizes<kWide, 0, 0, false>(g, size, st);
+    case 1: return launch_sizes<kWide, 0, 1, false>(g, size, st);
+    case 2: return launch_sizes<kWide, 1, 0, false>(g, size, st);
+    default: return launch_sizes<kWide, 1, 1, false>(g, size, st);
     }
 }
 

@@ -8,8 +8,6 @@
 namespace o2m {
 namespace {
 
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-
 struct Dest {
     uint8_t *values;
     int64_t ld;
@@ -32,23 +30,6 @@ __device__ inline void store_scale(const Dest &d, int64_t row, int64_t blk, uint
     else static_cast<uint8_t *>(d.scales)[i] = (uint8_t)held;
 }
 
-// Eight entries of one line from `x0`, of which `n` exist; zeros after them.
-template <class T, bool VEC>
-__device__ inline void load8(const T *x0, int n, float (&v)[8]) {
-    if (VEC && n >= 8) {
-        T t[8];
-        constexpr int parts = sizeof(T) * 8 / 16;
-#pragma unroll
-        for (int i = 0; i < parts; ++i)
-            reinterpret_cast<u32x4 *>(t)[i] = reinterpret_cast<const u32x4 *>(x0)[i];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = as_float(t[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < n ? as_float(x0[j]) : 0.0f;
-    }
-}
-
 __device__ inline void store_bytes(uint8_t *p, uint2 w, int n) {
     if (n >= 8) {
         *reinterpret_cast<uint2 *>(p) = w;
@@ -63,7 +44,7 @@ __device__ inline void store_bytes(uint8_t *p, uint2 w, int n) {
 // exchanges, and the maxima across lines and the bytes of the transposed operand
 // go through LDS (in 8-byte units of 8 lines, unit rg of position q in slot rg ^
 // (q / 8), which spreads both the writes and the reads over the banks).
-template <class T, bool VEC>
+template <class T>
 __global__ __launch_bounds__(256) void quantize_tile(QuantArgs g) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[128 * 128];
     __shared__ float tile_max[4];
@@ -76,7 +57,7 @@ __global__ __launch_bounds__(256) void quantize_tile(QuantArgs g) {
     for (int j = 0; j < 8; ++j) col_max[j] = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        load8<T, VEC>(static_cast<const T *>(g.X) + (int64_t)(p0 + i) * g.ld + q0, p0 + i < g.lines ? nq : 0, x[i]);
+        load8<T>(static_cast<const T *>(g.X) + (int64_t)(p0 + i) * g.ld + q0, p0 + i < g.lines ? nq : 0, x[i]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         float m = 0.0f;
@@ -174,16 +155,65 @@ __global__ __launch_bounds__(256) void quantize_tile(QuantArgs g) {
     }
 }
 
+// Along lines alone, in blocks of 1 x 128: 16 lanes hold a block, 8 entries each, and
+// nothing is shared.  PER blocks of a line, 16 lanes apart from one another, keep
+// that many loads in flight.
+template <class T, int PER>
+__global__ __launch_bounds__(256) void quantize_rows(QuantArgs g) {
+    const Dest &d = g.along;
+    const float top = d.format == O2M_FP8_E4M3 ? 448.0f : 57344.0f;
+    const int lane16 = threadIdx.x & 15;
+    const int64_t group = blockIdx.x * 16LL + (threadIdx.x >> 4);   // PER blocks of a line
+    const int groups = (g.tiles_q + PER - 1) / PER;
+    const int64_t p = group / groups;
+    if (p >= g.lines) return;
+    const int blk0 = (int)(group % groups) * PER;
+    const T *line = static_cast<const T *>(g.X) + p * g.ld;
+    float x[PER][8];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int q0 = (blk0 + i) * 128 + 8 * lane16;
+        load8<T>(line + q0, min(8, g.len - q0), x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, magnitude(x[i][j]));
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+        const Scale s = scale_of(m, d.format, d.scale_type);
+        const int q0 = (blk0 + i) * 128 + 8 * lane16, n = g.len - q0;
+        if (n <= 0) continue;
+        float y[4], z[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            y[j] = scaled(x[i][j], s.inv, top);
+            z[j] = scaled(x[i][4 + j], s.inv, top);
+        }
+        store_bytes(d.values + p * d.ld + q0, uint2{pack_fp8(y, d.format), pack_fp8(z, d.format)}, n);
+        if (lane16 == 0) store_scale(d, p, blk0 + i, s.held);
+    }
+}
+
 Dest dest_of(const o2m_fp8_operand *o) {
     if (!o) return {nullptr, 0, nullptr, 0, 0, 0, 0, 0};
     return {static_cast<uint8_t *>(o->values), o->ld, o->scales, o->s_row, o->s_blk, o->block, o->format, o->scale_type};
 }
 
+// Lines of many blocks are taken four at a time where that leaves enough
+// workgroups (8 a CU); a token's single line is taken block by block.
 template <class T>
-void launch_tiles(const QuantArgs &g, unsigned grid, hipStream_t st) {
-    const bool vec = (reinterpret_cast<uintptr_t>(g.X) % 16 == 0) && (g.ld * (int64_t)sizeof(T)) % 16 == 0;
-    if (vec) quantize_tile<T, true><<<grid, 256, 0, st>>>(g);
-    else quantize_tile<T, false><<<grid, 256, 0, st>>>(g);
+hipError_t launch(const QuantArgs &g, int64_t tiles, hipStream_t st) {
+    if (g.across.values || g.along.block != 1) {
+        quantize_tile<T><<<(unsigned)tiles, 256, 0, st>>>(g);
+        return hipGetLastError();
+    }
+    const int64_t by4 = ceil_div(g.lines * ceil_div(g.tiles_q, 4), 16), by1 = ceil_div((int64_t)g.lines * g.tiles_q, 16);
+    if (by1 > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (by4 >= 2048) quantize_rows<T, 4><<<(unsigned)by4, 256, 0, st>>>(g);
+    else quantize_rows<T, 1><<<(unsigned)by1, 256, 0, st>>>(g);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -195,11 +225,10 @@ hipError_t launch_quantize(int lines, int len, const void *X, int type, int64_t 
     if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
     const QuantArgs g = {X, ld, lines, len, (int)tiles_q, dest_of(along), dest_of(across)};
     switch (type) {
-    case O2M_TYPE_F32: launch_tiles<float>(g, (unsigned)tiles, st); break;
-    case O2M_TYPE_F16: launch_tiles<__half>(g, (unsigned)tiles, st); break;
-    default: launch_tiles<__hip_bfloat16>(g, (unsigned)tiles, st); break;
+    case O2M_TYPE_F32: return launch<float>(g, tiles, st);
+    case O2M_TYPE_F16: return launch<__half>(g, tiles, st);
+    default: return launch<__hip_bfloat16>(g, tiles, st);
     }
-    return hipGetLastError();
 }
 
 }  // namespace o2m

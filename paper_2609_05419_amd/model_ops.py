@@ -65,8 +65,12 @@ class Fp8Operand(NamedTuple):
     scales: torch.Tensor
 
 
+# the current device's index without torch.cuda's checks (a device tensor exists)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _here(x: torch.Tensor, name: str) -> None:
-    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+    if not x.is_cuda or x.get_device() != _current_device():
         raise ValueError(f"{name} must be a tensor on the current device")
 
 
@@ -150,11 +154,20 @@ def _scratch(nbytes: int, device, stream):
     return t, t.data_ptr(), nbytes
 
 
-def _fresh_operand(rows: int, k: int, block: int, dtype, scales: str, device, stream) -> Fp8Operand:
-    q = _empty((rows, (k + 15) // 16 * 16), torch.uint8, device, stream)[:, :k].view(dtype)
+def _strided(size, strides, dtype, device, stream):
+    if stream is None:
+        return torch.empty_strided(size, strides, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty_strided(size, strides, dtype=dtype, device=device)
+
+
+def _fresh_operand(rows: int, k: int, block: int, dtype, scales: str, device, stream):
+    """An operand to be written, and its C struct."""
+    ld = (k + 15) // 16 * 16
     r, kb = (rows if block == 1 else (rows + BLOCK - 1) // BLOCK), (k + BLOCK - 1) // BLOCK
-    s = _empty((kb, r), torch.uint8 if scales == "pow2" else torch.float32, device, stream)
-    return Fp8Operand(q, (s.view(torch.float8_e8m0fnu) if scales == "pow2" else s).t())
+    q = _strided((rows, k), (ld, 1), dtype, device, stream)
+    s = _strided((r, kb), (1, max(r, 1)), _SCALE_DTYPES[scales], device, stream)
+    return Fp8Operand(q, s), _Operand(q.data_ptr(), ld, s.data_ptr(), 1, r, block, _FORMATS[dtype], _SCALES[scales])
 
 
 def _quantize_args(block, dtype, scales):
@@ -167,19 +180,11 @@ def _quantize_args(block, dtype, scales):
     return block[0]
 
 
-def _quantize(X, Q, Qt, name, stream):
-    t = _type_of(X, "X")
-    order, ld = _matrix(X, "X")
-    rows, k = X.shape
-    structs = []
-    for what, x, shape in (("out", Q, (rows, k)), ("transposed out", Qt, (k, rows))):
-        if x is None:
-            structs.append(None)
-            continue
-        if tuple(x[0].shape) != shape:
-            raise ValueError(f"{what}: values must be of shape {shape}, got {tuple(x[0].shape)}")
-        structs.append(ctypes.byref(_operand(x, what)))
-    _check(_L.o2m_quantize_fp8(rows, k, X.data_ptr(), t, order, ld, structs[0], structs[1], _stream(stream)), name)
+def _written(out, shape, what):
+    """The C struct of an operand given to be written."""
+    if tuple(out[0].shape) != shape:
+        raise ValueError(f"{what}: values must be of shape {shape}, got {tuple(out[0].shape)}")
+    return _operand(out, what)
 
 
 def quantize_fp8(X: torch.Tensor, block=(1, 128), dtype=torch.float8_e4m3fn, scales: str = "pow2", out=None,
@@ -193,10 +198,15 @@ def quantize_fp8(X: torch.Tensor, block=(1, 128), dtype=torch.float8_e4m3fn, sca
     nearest, ties to even, and Inf and NaN become NaN.  ``quantize_fp8(X.t())``
     is the operand of the transpose.  ``out``: an operand to write into, of any
     format and kind of scales (the other arguments are then not used)."""
+    t = _type_of(X, "X")
+    b = _quantize_args(block, dtype, scales) if out is None else 0
+    order, ld = _matrix(X, "X")
+    rows, k = X.shape
     if out is None:
-        b = _quantize_args(block, dtype, scales)
-        out = _fresh_operand(X.size(0), X.size(1), b, dtype, scales, X.device, stream) if X.dim() == 2 else out
-    _quantize(X, out, None, "quantize_fp8", stream)
+        out, q = _fresh_operand(rows, k, b, dtype, scales, X.device, stream)
+    else:
+        q = _written(out, (rows, k), "out")
+    _check(_L.o2m_quantize_fp8(rows, k, X.data_ptr(), t, order, ld, q, None, _stream(stream)), "quantize_fp8")
     return out
 
 
@@ -205,14 +215,17 @@ def quantize_fp8_pair(X: torch.Tensor, block=(1, 128), dtype=torch.float8_e4m3fn
     """The operands of X and of its transpose from one reading of X (what a
     layer's forward product and its backward products take of X, W or dY).
     ``out``: a pair of operands to write into."""
+    t = _type_of(X, "X")
+    b = _quantize_args(block, dtype, scales) if out is None else 0
+    order, ld = _matrix(X, "X")
+    rows, k = X.shape
     if out is None:
-        b = _quantize_args(block, dtype, scales)
-        if X.dim() != 2:
-            raise ValueError(f"X must be a matrix, got {X.dim()} dimensions")
-        rows, k = X.shape
-        out = (_fresh_operand(rows, k, b, dtype, scales, X.device, stream),
-               _fresh_operand(k, rows, b, dtype, scales, X.device, stream))
-    _quantize(X, out[0], out[1], "quantize_fp8_pair", stream)
+        first, q = _fresh_operand(rows, k, b, dtype, scales, X.device, stream)
+        second, qt = _fresh_operand(k, rows, b, dtype, scales, X.device, stream)
+        out = (first, second)
+    else:
+        q, qt = _written(out[0], (rows, k), "out"), _written(out[1], (k, rows), "transposed out")
+    _check(_L.o2m_quantize_fp8(rows, k, X.data_ptr(), t, order, ld, q, qt, _stream(stream)), "quantize_fp8_pair")
     return out
 
 
@@ -240,7 +253,7 @@ def gemm_fp8(A, B, dtype=torch.bfloat16, out: torch.Tensor | None = None, accumu
     t = _type_of(out, "out")
     order, ld = _matrix(out, "out")
     ws, at, nbytes = _scratch(_L.o2m_gemm_fp8_workspace(m, n, k), out.device, stream)
-    _check(_L.o2m_gemm_fp8(m, n, k, ctypes.byref(a), ctypes.byref(b), out.data_ptr(), t, order, ld, int(accumulate), at,
+    _check(_L.o2m_gemm_fp8(m, n, k, a, b, out.data_ptr(), t, order, ld, int(accumulate), at,
                            nbytes, _stream(stream)), "gemm_fp8")
     return out
 
@@ -266,7 +279,7 @@ def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None)
     if order != b"R":
         raise ValueError("out must be row-major")
     ws, at, nbytes = _scratch(_L.o2m_linear_fp8_workspace(tokens, n, k), out.device, stream)
-    _check(_L.o2m_linear_fp8(tokens, n, k, X.data_ptr(), t, ldx, ctypes.byref(w), out.data_ptr(), ldy, at, nbytes,
+    _check(_L.o2m_linear_fp8(tokens, n, k, X.data_ptr(), t, ldx, w, out.data_ptr(), ldy, at, nbytes,
                              _stream(stream)), "linear_fp8")
     return out
 

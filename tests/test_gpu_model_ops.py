@@ -138,11 +138,12 @@ def test_gemm(o2m, m, n, k, scales):
 
 
 @pytest.mark.parametrize("m,n,k", [(1290, 1601, 128), (1290, 1601, 97), (1537, 1283, 300), (1536, 2048, 256), (1400, 1900, 1041),
-                                   (8, 8200, 700), (9000, 130, 2064)])
+                                   (8, 8200, 700), (9000, 130, 2064), (2100, 2000, 200), (2065, 2100, 333),
+                                   (3700, 3601, 128), (3700, 3601, 97), (3601, 3700, 300), (3590, 3800, 1041), (140, 60001, 264)])
 @pytest.mark.parametrize("scales", ["pow2", "float32"])
 def test_gemm_large(o2m, m, n, k, scales):
-    """Enough tiles of 256 x 256 for the kernels of large products: one stage and
-    many, odd and even numbers of them, ends of k within 16 bytes, ragged edges."""
+    """Enough tiles for the kernels of larger products: one stage and many, odd and
+    even numbers of them, ends of k within 16 bytes, ragged edges."""
     for i, (ba, bb, fa, fb, dtype) in enumerate([(1, 128, E4M3, E4M3, torch.bfloat16), (1, 1, E5M2, E4M3, torch.float16),
                                                  (128, 1, E4M3, E5M2, torch.bfloat16), (128, 128, E5M2, E5M2, torch.float32)]):
         a, b = matrix(m, k, 20 + i, spread=0.5), matrix(n, k, 40 + i, spread=0.5)
