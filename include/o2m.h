@@ -353,7 +353,8 @@ size_t o2m_linear_fp8_workspace(int tokens, int n, int k);
    are held in fp16 with one power-of-two scale (11 bits, 3 more than the
    result), fp32 and fp16 ones in two fp16 parts (22 bits).  The held range
    asks for singular values below 4 in every step, which the usual
-   coefficients keep far below 2.  Inf or NaN in G gives NaN in the whole
+   coefficients keep far below 2.  A matrix has at most 2^29 entries (its sizes
+   rounded up to multiples of 64) and a side of at most 2^21.  Inf or NaN in G gives NaN in the whole
    matrix.  O must not overlap G, except to be G in the same layout.  Argument
    errors: -1 batch, -2 rows, -3 cols, -4 G, -5 order_g, -6 ldg, -7 stride_g,
    -8 O, -9 order_o, -10 ldo, -11 stride_o, -12 type, O2M_ERR_STEPS steps,

@@ -177,9 +177,9 @@ o2m_status o2m_orthogonalize(int batch, int rows, int cols, const void *G, char 
     if (!any) return O2M_OK;
     const bool tall = rows > cols;
     const int r = tall ? cols : rows, c = tall ? rows : cols;
-    // offsets within a tile, and the tiles of a launch
-    const int64_t rt = ceil_div(r, 128), ct = ceil_div(c, 128);
-    if (c > (1 << 21) || batch > 65535 || 4 * rt * ct > 0x7FFFFFFF / (int64_t)batch) return O2M_ERR_SIZE;
+    // offsets within a tile, and within the two parts of a matrix; the tiles of a launch
+    const int64_t rt = ceil_div(r, 64), ct = ceil_div(c, 64);
+    if (c > (1 << 21) || (rt * ct) << 12 > (1 << 29) || batch > 65535 || 256 * rt * ct > 0x7FFFFFFF / (int64_t)batch) return O2M_ERR_SIZE;
     const o2m_status s = check_workspace(ortho_workspace(batch, r, c, type), workspace, workspace_bytes);
     if (s != O2M_OK) return s;
     OrthoArgs a;

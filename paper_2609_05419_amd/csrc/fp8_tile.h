@@ -108,12 +108,12 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
 #pragma unroll
         for (int c = 0; c < T::kCopyA; ++c) {
             const int q = wave * T::kCopyA + c;
-            copy_rows<0>(ra, buf + q * 1024, lane, q, (int)g.a.ld, kb, left);
+            copy_rows<0>(ra, buf + q * 1024, lane, q, (int)g.a.ld, kb * kStageRowBytes, left);
         }
 #pragma unroll
         for (int c = 0; c < T::kCopyB; ++c) {
             const int q = wave * T::kCopyB + c;
-            copy_rows<2>(rb, buf + T::kTm * kStageRowBytes + q * 1024, lane, q, (int)g.b.ld, kb, left);
+            copy_rows<2>(rb, buf + T::kTm * kStageRowBytes + q * 1024, lane, q, (int)g.b.ld, kb * kStageRowBytes, left);
         }
     };
     // (threads past the rows fetch the last row's)

@@ -93,7 +93,8 @@ struct Fp8Src {
     int ld_a, ld_b, kbytes;
     __device__ inline __amdgpu_buffer_rsrc_t a(int) const { return ra; }
     __device__ inline __amdgpu_buffer_rsrc_t b(int) const { return rb; }
-    __device__ inline int k(int s) const { return s; }
+    __device__ inline int at_a(int s) const { return s * kStageRowBytes; }
+    __device__ inline int at_b(int s) const { return s * kStageRowBytes; }
     __device__ inline int left(int s) const { return kbytes - s * kBlockK; }
 };
 

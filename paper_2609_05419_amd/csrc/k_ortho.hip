@@ -1,30 +1,33 @@
 // The orthogonalised update (include/o2m.h: o2m_orthogonalize):
 //
-//   X = G / (||G|| + eps);  steps x:  A = X X^T, B = b A + c A^2, X <- a X + B X
+//   X = G / (||G|| + eps);  steps x:  A = X X^T, B = a I + b A + c A^2, X <- B X
 //
 // on the work matrix X (r x c, r <= c, G transposed where it is tall).  Three
 // products per step: A and A^2 symmetric, so half their tiles are computed and
-// mirrored, then B X with a X added as it is stored.
+// mirrored, then B X.  (With a in B rather than a X added to the last product, that
+// one reads nothing but its operands, and B's rounding, relative to a + b s^2 + c
+// s^4 rather than to b s^2 + c s^4, is if anything the smaller one.)
 //
-// Held numbers.  |X| <= s_max in every entry, A <= s_max^2, and of the size of 1 /
+// Held numbers.  |X| <= s_max in every entry, A <= s_max^2, and X of the size of 1 /
 // sqrt(c) in the end: matrices are held in fp16, as X 2^14, A 2^11 and B 2^6, which
-// leaves room for singular values up to 4 and keeps fp16's smallest numbers
-// 2^-24 far below what counts.  For bf16 updates one fp16 part is kept, whose 11
+// leaves room for singular values up to 4 (and B up to 1000) and keeps fp16's
+// smallest numbers 2^-24 far below what counts.  For bf16 updates one fp16 part is kept, whose 11
 // bits put the held matrices' roundings below the result's own; fp32 and fp16
 // updates keep the rest in a second fp16 part, and multiply lo hi + hi lo + hi
 // hi, all summed in fp32.  What is left out, lo lo, is 2^-24 of the product.
 //
-// Layout.  All held matrices are padded with zeros to multiples of 128, so no
-// product has a ragged edge.  X is kept both as it is (the rows that A
+// Layout.  All held matrices are padded with zeros to multiples of 64, so no
+// product has a ragged edge within a stage.  X is kept both as it is (the rows that A
 // multiplies) and transposed (the rows that B X multiplies); the product that
 // makes it writes both.
 //
-// Products with enough 256 x 256 tiles to go round take the pipeline of
-// mfma_pipe.h and write from it; the others take tiles of 128 x 128, split along
-// k until they fill the part, whose fp32 sums a second kernel adds up and writes.
+// Products take the pipeline of mfma_pipe.h or smaller tiles (plan_product); those
+// with too few tiles are split along k, and a second kernel adds the fp32 sums
+// up and writes.
 //
-// Bound: fp16 MFMA; 3 r^2 c + r^3 multiply-adds a step, halves counted once, and
+// Bound: fp16 MFMA; 1.5 r^2 c + 0.5 r^3 multiply-adds a step, halves counted once, and
 // three times that for two parts.
+#include "fp8_round.h"
 #include "mfma_pipe.h"
 #include "mfma_tiles.h"
 #include "model_internal.h"
@@ -42,67 +45,73 @@ typedef _Float16 f16;
 typedef f16 v8f16 __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
 
-constexpr int kPad = 128;
+constexpr int kPad = 64;
 constexpr int kScaleX = 14, kScaleA = 11, kScaleB = 6;
-constexpr int kParts = 256;   // partial sums of the norm, per matrix
+constexpr int kParts = 1024;   // partial sums of the norm, at most, per matrix
 
 struct Planes {
-    f16 *hi, *lo;     // lo: null when one part is kept
+    f16 *hi;
+    int64_t lo;       // the second part, elements after the first; 0 when one is kept
     int64_t pitch;    // elements of a row
-    int64_t batch;    // elements of a matrix
+    int64_t batch;    // from matrix to matrix, both parts
 };
 
-__device__ inline float load_any(const void *p, int64_t i, int type) {
-    if (type == O2M_TYPE_F32) return static_cast<const float *>(p)[i];
-    if (type == O2M_TYPE_F16) return __half2float(static_cast<const __half *>(p)[i]);
-    return __bfloat162float(static_cast<const __hip_bfloat16 *>(p)[i]);
-}
 __device__ inline void store_any(void *p, int64_t i, int type, float v) {
     if (type == O2M_TYPE_F32) static_cast<float *>(p)[i] = v;
     else if (type == O2M_TYPE_F16) static_cast<__half *>(p)[i] = __float2half(v);
     else static_cast<__hip_bfloat16 *>(p)[i] = __float2bfloat16(v);
 }
 
-// An entry held in one or two parts, and 8 neighbouring ones.
+// An entry held in one or two parts.
 template <bool SPLIT>
 __device__ inline float held(const Planes &m, int64_t i) {
-    return SPLIT ? (float)m.hi[i] + (float)m.lo[i] : (float)m.hi[i];
+    return SPLIT ? (float)m.hi[i] + (float)m.hi[i + m.lo] : (float)m.hi[i];
 }
-template <bool SPLIT>
-__device__ inline void hold(const Planes &m, int64_t i, float v) {
-    const f16 hi = (f16)v;
-    m.hi[i] = hi;
-    if (SPLIT) m.lo[i] = (f16)(v - (float)hi);
-}
-template <bool SPLIT>
-__device__ inline v8f held8(const Planes &m, int64_t i) {
-    v8f v = __builtin_convertvector(*reinterpret_cast<const v8f16 *>(m.hi + i), v8f);
-    if (SPLIT) v += __builtin_convertvector(*reinterpret_cast<const v8f16 *>(m.lo + i), v8f);
+// N neighbouring entries.
+template <bool SPLIT, int N, class V>
+__device__ inline V held_run(const Planes &m, int64_t i) {
+    typedef f16 vf16 __attribute__((ext_vector_type(N)));
+    V v = __builtin_convertvector(*reinterpret_cast<const vf16 *>(m.hi + i), V);
+    if (SPLIT) v += __builtin_convertvector(*reinterpret_cast<const vf16 *>(m.hi + m.lo + i), V);
     return v;
 }
-template <bool SPLIT>
-__device__ inline void hold8(const Planes &m, int64_t i, const v8f &v) {
-    const v8f16 hi = __builtin_convertvector(v, v8f16);
-    *reinterpret_cast<v8f16 *>(m.hi + i) = hi;
-    if (SPLIT)
-        *reinterpret_cast<v8f16 *>(m.lo + i) = __builtin_convertvector(v - __builtin_convertvector(hi, v8f), v8f16);
+template <bool SPLIT, int N, class V>
+__device__ inline void hold_run(const Planes &m, int64_t i, const V &v) {
+    typedef f16 vf16 __attribute__((ext_vector_type(N)));
+    const vf16 hi = __builtin_convertvector(v, vf16);
+    *reinterpret_cast<vf16 *>(m.hi + i) = hi;
+    if (SPLIT) *reinterpret_cast<vf16 *>(m.hi + m.lo + i) = __builtin_convertvector(v - __builtin_convertvector(hi, V), vf16);
+}
+// Eight neighbouring entries, of which the first n exist, zeros after them.
+__device__ inline v8f load_some(const void *p, int64_t i, int n, int type) {
+    float v[8];
+    if (type == O2M_TYPE_F32) load8(static_cast<const float *>(p) + i, n, v);
+    else if (type == O2M_TYPE_F16) load8(static_cast<const __half *>(p) + i, n, v);
+    else load8(static_cast<const __hip_bfloat16 *>(p) + i, n, v);
+    return v8f{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
 }
 
-// Sums of squares in fp64, a fixed part per workgroup, so that every run adds
-// in the same order.
-struct NormArgs {
+// G of a batch as lines of contiguous entries.
+struct Lines {
     const void *G;
-    int64_t g_outer, g_batch;
-    int outer, inner, type;
-    double *parts;
+    int64_t line, batch;   // strides
+    int lines, len, type;
 };
-__global__ __launch_bounds__(256) void norm_parts(NormArgs g) {
+
+// Sums of squares in fp64: part z adds up the runs of 8 entries z, z + parts, ..,
+// its threads in a fixed order, so that every run of the call adds in the same one.
+__global__ __launch_bounds__(256) void norm_parts(Lines g, int parts, double *out) {
     __shared__ double sums[256];
-    const int64_t total = (int64_t)g.outer * g.inner, base = (int64_t)blockIdx.y * g.g_batch;
+    const unsigned per_line = (unsigned)(g.len + 7) / 8;
+    const int64_t runs = (int64_t)per_line * g.lines, base = blockIdx.y * g.batch;
     double s = 0.0;
-    for (int64_t t = blockIdx.x * 256LL + threadIdx.x; t < total; t += kParts * 256LL) {
-        const double v = load_any(g.G, base + t / g.inner * g.g_outer + t % g.inner, g.type);
-        s += v * v;
+    for (int64_t t = blockIdx.x * 256LL + threadIdx.x; t < runs; t += parts * 256LL) {
+        // (the quotient of a line's runs: 32 bits where they suffice)
+        const int64_t p = runs <= 0xFFFFFFFFLL ? (int64_t)((unsigned)t / per_line) : t / per_line;
+        const int q = (int)(t - p * per_line) * 8;
+        const v8f v = load_some(g.G, base + p * g.line + q, g.len - q, g.type);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += (double)v[j] * (double)v[j];
     }
     sums[threadIdx.x] = s;
     __syncthreads();
@@ -110,64 +119,78 @@ __global__ __launch_bounds__(256) void norm_parts(NormArgs g) {
         if (threadIdx.x < w) sums[threadIdx.x] += sums[threadIdx.x + w];
         __syncthreads();
     }
-    if (threadIdx.x == 0) g.parts[(int64_t)blockIdx.y * kParts + blockIdx.x] = sums[0];
+    if (threadIdx.x == 0) out[(int64_t)blockIdx.y * kParts + blockIdx.x] = sums[0];
 }
 
-struct PrepArgs {
-    const void *G;
-    int64_t g_row, g_col, g_batch;
-    int r, c, type;
-    const double *parts;
-    double eps;
-    double scale;    // 2^s
-    Planes x, t;     // X (r x c) and its transpose, padded
-    int tiles_c;
-};
-// X 2^s and its transpose, 64 x 64 entries per workgroup.
-template <bool SPLIT>
-__global__ __launch_bounds__(256) void prepare_x(PrepArgs g) {
-    __shared__ float tile[64][65];
-    __shared__ double sums[256];
-    const int tid = threadIdx.x, b = blockIdx.y;
-    sums[tid] = g.parts[(int64_t)b * kParts + tid];
+// scale / (norm + eps) from the parts, for the whole workgroup; NaN when the norm is
+// not finite.
+__device__ inline double inverse_norm(const double *parts, int count, double eps, double scale, double *sums) {
+    const int tid = threadIdx.x;
+    double s = 0.0;
+    for (int i = tid; i < count; i += 256) s += parts[i];
+    sums[tid] = s;
     __syncthreads();
     for (int w = 128; w > 0; w >>= 1) {
         if (tid < w) sums[tid] += sums[tid + w];
         __syncthreads();
     }
     const double norm = sqrt(sums[0]);
-    // Inf and NaN anywhere: NaN everywhere
-    const double inv = norm <= 1.7e308 ? g.scale / (norm + g.eps) : (double)NAN;
-    const int i0 = blockIdx.x / g.tiles_c * 64, j0 = blockIdx.x % g.tiles_c * 64;
-    const bool along_c = g.g_col == 1;
-    for (int t = tid; t < 64 * 64; t += 256) {
-        const int i = along_c ? t >> 6 : t & 63, j = along_c ? t & 63 : t >> 6;
-        float v = 0.0f;
-        if (i0 + i < g.r && j0 + j < g.c)
-            v = (float)((double)load_any(g.G, b * g.g_batch + (i0 + i) * g.g_row + (j0 + j) * g.g_col, g.type) * inv);
-        tile[i][j] = v;
+    return norm <= 1.7e308 ? scale / (norm + eps) : (double)NAN;
+}
+
+struct PrepArgs {
+    Lines g;
+    const double *parts;
+    int count;
+    double eps, scale;   // scale: 2^kScaleX
+    Planes along, across;   // the lines of G, and their transpose, padded
+    int tiles_q;
+};
+// G / (norm + eps) held, and its transpose, 64 x 64 entries per workgroup.
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void prepare_x(PrepArgs g) {
+    __shared__ float tile[64][65];
+    __shared__ double sums[256];
+    const int tid = threadIdx.x, b = blockIdx.y;
+    const double inv = inverse_norm(g.parts + (int64_t)b * kParts, g.count, g.eps, g.scale, sums);
+    const int p0 = blockIdx.x / g.tiles_q * 64, q0 = blockIdx.x % g.tiles_q * 64;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int p = 32 * h + (tid >> 3), q = (tid & 7) * 8;
+        const int n = p0 + p < g.g.lines ? min(8, g.g.len - q0 - q) : 0;
+        v8f v = load_some(g.g.G, b * g.g.batch + (p0 + p) * g.g.line + q0 + q, n, g.g.type);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = j < n ? (float)((double)v[j] * inv) : 0.0f;   // (padding stays zero under a NaN)
+            tile[p][q + j] = v[j];
+        }
+        hold_run<SPLIT, 8>(g.along, b * g.along.batch + (p0 + p) * g.along.pitch + q0 + q, v);
     }
     __syncthreads();
-    for (int t = tid; t < 64 * 64; t += 256) {
-        const int p = t >> 6, q = t & 63;
-        hold<SPLIT>(g.x, b * g.x.batch + (i0 + p) * g.x.pitch + j0 + q, tile[p][q]);
-        hold<SPLIT>(g.t, b * g.t.batch + (j0 + p) * g.t.pitch + i0 + q, tile[q][p]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int q = 32 * h + (tid >> 3), p = (tid & 7) * 8;
+        v8f v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = tile[p + i][q];
+        hold_run<SPLIT, 8>(g.across, b * g.across.batch + (q0 + q) * g.across.pitch + p0 + p, v);
     }
 }
 
 enum Product { kGram, kPoly, kUpdate, kLast };
 constexpr bool symmetric(Product k) { return k == kGram || k == kPoly; }
 
-// D = add E + mul P Q^T, of rows x cols entries (padded).
+// D = diag I + add E + mul P Q^T (kPoly; the others: mul P Q^T), of rows x cols
+// entries (padded).
 struct ProductArgs {
     Planes p, q;
-    Planes e, et;       // kPoly: A twice; kUpdate, kLast: X and its transpose
+    Planes e;           // kPoly: A
     Planes d, dt;       // D and its transpose (kGram, kPoly: the same matrix)
     int rows, cols;
     int kblocks;        // stages of 64
     int mt, nt, tiles;  // tiles of the launch's size; per matrix
     int batch, chunk;   // chunk: tiles of the whole launch per XCD
-    float add, mul;
+    float diag, add, mul;
     float *parts;       // split launches: sums [split][batch][rows][cols]
     int splits, per;    // stages of a split
     void *O;            // kLast: where the r x c result goes
@@ -187,47 +210,55 @@ __device__ inline void triangle_tile(int t, int &ti, int &tj) {
 // Matrix and tile of slot t of a launch; tiles of one matrix in groups of 8
 // tile-rows (tile_schedule.h), or a triangle.
 template <Product KIND>
-__device__ inline bool tile_at(const ProductArgs &g, int64_t t, int &b, int &ti, int &tj) {
-    b = (int)(t / g.tiles);
+__device__ inline bool tile_at(const ProductArgs &g, int64_t t, int mt, int nt, int tiles, int &b, int &ti, int &tj) {
+    b = (int)(t / tiles);
     if (b >= g.batch) return false;
-    const int in = (int)(t % g.tiles);
+    const int in = (int)(t % tiles);
     if (symmetric(KIND)) {
         triangle_tile(in, ti, tj);
         return true;
     }
-    const TileCoord c = tile_of(0, in, g.mt, g.nt, g.tiles, 0);
+    const TileCoord c = tile_of(0, in, mt, nt, tiles, 0);
     ti = c.ti;
     tj = c.tj;
     return true;
 }
 
-// The stages of a product: kblocks of hi hi, before them, with two parts, those
-// of lo hi and hi lo.
+// The stages [first, first + total) of a product: kblocks of hi hi, before them,
+// with two parts, those of lo hi and hi lo.
 template <bool SPLIT>
 struct HalfSrc {
-    __amdgpu_buffer_rsrc_t p_hi, p_lo, q_hi, q_lo;
-    int ld_a, ld_b, kblocks, total;
-    __device__ inline HalfSrc(const ProductArgs &g, int b, int i0, int j0, int tile) {
+    // one descriptor for both parts: the second lies a fixed distance on (so rows
+    // past the last one read what follows, which only rows that are not written
+    // see, and not zeros)
+    __amdgpu_buffer_rsrc_t rp, rq;
+    int ld_a, ld_b, lo_a, lo_b, kblocks, first, total;
+    __device__ inline HalfSrc(const ProductArgs &g, int b, int i0, int j0, int tile_m, int tile_n, int z) {
         kblocks = g.kblocks;
-        total = SPLIT ? 3 * kblocks : kblocks;
+        first = z * g.per;
+        total = min(g.per, (SPLIT ? 3 : 1) * kblocks - first);
         ld_a = (int)g.p.pitch * 2;
         ld_b = (int)g.q.pitch * 2;
-        auto rows = [&](const f16 *m, const Planes &of, int row0, int all, int ld) {
-            return rows_of(reinterpret_cast<const uint8_t *>(m + b * of.batch + row0 * of.pitch), min(tile, all - row0), ld,
-                           kblocks * kStageRowBytes);
+        lo_a = (int)g.p.lo * 2;
+        lo_b = (int)g.q.lo * 2;
+        auto rows = [&](const Planes &of, int row0, int all, int tile, int ld, int lo) {
+            const int extent = lo + (min(tile, all - row0) - 1) * ld + kblocks * kStageRowBytes;
+            return __builtin_amdgcn_make_buffer_rsrc(of.hi + b * of.batch + row0 * of.pitch, (short)0, extent, 0x00020000);
         };
-        p_hi = rows(g.p.hi, g.p, i0, g.rows, ld_a);
-        q_hi = rows(g.q.hi, g.q, j0, g.cols, ld_b);
-        if (SPLIT) {
-            p_lo = rows(g.p.lo, g.p, i0, g.rows, ld_a);
-            q_lo = rows(g.q.lo, g.q, j0, g.cols, ld_b);
-        }
+        rp = rows(g.p, i0, g.rows, tile_m, ld_a, SPLIT ? lo_a : 0);
+        rq = rows(g.q, j0, g.cols, tile_n, ld_b, SPLIT ? lo_b : 0);
     }
-    __device__ inline __amdgpu_buffer_rsrc_t a(int s) const { return SPLIT && s < kblocks ? p_lo : p_hi; }
-    __device__ inline __amdgpu_buffer_rsrc_t b(int s) const {
-        return SPLIT && s >= kblocks && s < 2 * kblocks ? q_lo : q_hi;
+    __device__ inline __amdgpu_buffer_rsrc_t a(int) const { return rp; }
+    __device__ inline __amdgpu_buffer_rsrc_t b(int) const { return rq; }
+    // byte offsets of stage s: passes lo hi, hi lo, hi hi
+    __device__ inline int at_a(int s) const {
+        const int at = first + s, pass = SPLIT ? (at >= kblocks) + (at >= 2 * kblocks) : 2;
+        return (SPLIT ? at - pass * kblocks : at) * kStageRowBytes + (SPLIT && pass == 0 ? lo_a : 0);
     }
-    __device__ inline int k(int s) const { return !SPLIT || s < kblocks ? s : s < 2 * kblocks ? s - kblocks : s - 2 * kblocks; }
+    __device__ inline int at_b(int s) const {
+        const int at = first + s, pass = SPLIT ? (at >= kblocks) + (at >= 2 * kblocks) : 2;
+        return (SPLIT ? at - pass * kblocks : at) * kStageRowBytes + (SPLIT && pass == 1 ? lo_b : 0);
+    }
     __device__ inline int left(int s) const { return s < total ? kStageRowBytes : 0; }
 };
 
@@ -248,150 +279,191 @@ struct HalfOp {
     }
 };
 
-// The first n of eight values.
-template <class T, class V>
+// The first n of N values of the result.
+template <int N, class T, class V>
 __device__ inline void store_some(T *p, const V &v, int n) {
-    if (n >= 8 && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
-        *reinterpret_cast<V *>(p) = v;
+    if (n >= N) {
+        __builtin_memcpy(p, &v, sizeof(T) * N);
     } else {
-        each<8>([&](auto J) {
+        each<N>([&](auto J) {
             if (J < n) p[J] = v[(int)J];
         });
     }
 }
 
-// Eight outputs of row `row`, columns col .. col + 7 (T: of column `col`, rows row ..
-// row + 7), given the sums.
-template <bool SPLIT, Product KIND, bool T>
-__device__ inline void emit(const ProductArgs &g, int b, int row, int col, v8f v) {
+// N outputs of row `row`, columns col .. (T: of column `col`, rows row ..), given the
+// sums.
+template <bool SPLIT, Product KIND, bool T, int N, class V>
+__device__ inline void emit(const ProductArgs &g, int b, int row, int col, V v) {
+    typedef f16 vf16 __attribute__((ext_vector_type(N)));
+    typedef __bf16 vbf16 __attribute__((ext_vector_type(N)));
     const int first = T ? row : col, line = T ? col : row;
     if (row >= g.rows || col >= g.cols) return;
     v *= g.mul;
-    if (KIND != kGram) {
-        const Planes &e = T ? g.et : g.e;
-        v += g.add * held8<SPLIT>(e, b * e.batch + line * e.pitch + first);
+    if (KIND == kPoly) {
+        v += g.add * held_run<SPLIT, N, V>(g.e, b * g.e.batch + line * g.e.pitch + first);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] += first + j == line ? g.diag : 0.0f;
     }
     if (KIND != kLast) {
         const Planes &d = T ? g.dt : g.d;
-        hold8<SPLIT>(d, b * d.batch + line * d.pitch + first, v);
+        hold_run<SPLIT, N, V>(d, b * d.batch + line * d.pitch + first, v);
         return;
     }
-    const int lines = T ? g.c : g.r, n = min(8, (T ? g.r : g.c) - first);
-    if (line >= lines) return;
+    const int n = min(N, (T ? g.r : g.c) - first);
+    if (line >= (T ? g.c : g.r) || n <= 0) return;
     const int64_t at = b * g.o_batch + row * g.o_row + col * g.o_col;
     v *= g.out_scale;
-    if (g.type == O2M_TYPE_F32) store_some(static_cast<float *>(g.O) + at, v, n);
-    else if (g.type == O2M_TYPE_F16) store_some(static_cast<f16 *>(g.O) + at, __builtin_convertvector(v, v8f16), n);
-    else store_some(static_cast<__bf16 *>(g.O) + at, __builtin_convertvector(v, v8bf16), n);
+    if (g.type == O2M_TYPE_F32) store_some<N>(static_cast<float *>(g.O) + at, v, n);
+    else if (g.type == O2M_TYPE_F16) store_some<N>(static_cast<f16 *>(g.O) + at, __builtin_convertvector(v, vf16), n);
+    else store_some<N>(static_cast<__bf16 *>(g.O) + at, __builtin_convertvector(v, vbf16), n);
+}
+
+// Which directions a product is written in.  A symmetric one: a tile on the
+// diagonal holds both halves already, another is mirrored; X: both ways, the
+// result in the one in which it is contiguous.
+template <Product KIND>
+__device__ inline bool writes_rows(const ProductArgs &g) { return KIND != kLast || g.o_col == 1; }
+template <Product KIND>
+__device__ inline bool writes_across(const ProductArgs &g, int ti, int tj) {
+    return symmetric(KIND) ? ti != tj : KIND != kLast || g.o_col != 1;
+}
+
+__device__ inline float *part_of(const ProductArgs &g, int z, int b) {
+    return g.parts + ((int64_t)z * g.batch + b) * g.rows * g.cols;
 }
 
 template <bool SPLIT, Product KIND>
 __global__ __launch_bounds__(256, 1) void product_pipe(ProductArgs g) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kPipeLds];
     const PipeWave w = pipe_wave(lds);
+    const int64_t slot = (int64_t)(blockIdx.x & 7) * g.chunk + (blockIdx.x >> 3);
+    const int z = (int)(slot % g.splits);
     int b, ti, tj;
-    if (!tile_at<KIND>(g, (int64_t)(blockIdx.x & 7) * g.chunk + (blockIdx.x >> 3), b, ti, tj)) return;
+    if (!tile_at<KIND>(g, slot / g.splits, g.mt, g.nt, g.tiles, b, ti, tj)) return;
     const int i0 = ti * kPipeTile, j0 = tj * kPipeTile;
-    const HalfSrc<SPLIT> src(g, b, i0, j0, kPipeTile);
+    const HalfSrc<SPLIT> src(g, b, i0, j0, kPipeTile, kPipeTile, z);
     HalfOp op;
     v4f acc[8][8];
     pipe_run(w, op, src, src.total, acc);
-    // a diagonal tile holds both halves already, an off-diagonal one is mirrored
-    const bool rows = KIND != kLast || g.o_col == 1;
-    const bool across = symmetric(KIND) ? ti != tj : KIND != kLast || !rows;
-    if (rows)
-        pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, false>(g, b, i0 + row, j0 + col, v); });
-    if (across)
-        pipe_results<true>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, true>(g, b, i0 + row, j0 + col, v); });
+    if (g.splits > 1) {
+        float *part = part_of(g, z, b);
+        pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) {
+            if (i0 + row < g.rows && j0 + col < g.cols)
+                *reinterpret_cast<v8f *>(part + (int64_t)(i0 + row) * g.cols + j0 + col) = v;
+        });
+        return;
+    }
+    if (writes_rows<KIND>(g))
+        pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, false, 8>(g, b, i0 + row, j0 + col, v); });
+    if (writes_across<KIND>(g, ti, tj))
+        pipe_results<true>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, true, 8>(g, b, i0 + row, j0 + col, v); });
 }
 
-// fp32 sums of a part of the stages on 128 x 128, by 2 x 2 waves of 4 x 4 blocks;
-// two stage buffers, two workgroups per CU.  Columns of a wave are 4 q + j (block
-// j, q = lane % 16), so that a lane's 4 blocks are 4 neighbouring columns.
-template <bool SPLIT, Product KIND>
-__global__ __launch_bounds__(256, 2) void product_parts(ProductArgs g) {
-    constexpr int T = kPad, kBuf = 2 * T * kStageRowBytes;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kBuf];
+// Smaller tiles: WR x WC waves of M x 4 blocks, a ring of S stage buffers with S - 1
+// stages on their way.  Rows of a wave are 16 i + q (block i, q = lane % 16),
+// columns 4 q + j: a lane holds 4 neighbouring columns (its blocks j) of 4
+// neighbouring rows (an accumulator), so it writes 8 bytes in either direction.
+template <bool SPLIT, Product KIND, int WR, int WC, int M, int S>
+__global__ __launch_bounds__(64 * WR * WC, 2) void product_tile(ProductArgs g) {
+    constexpr int kWaves = WR * WC, kTm = WR * M * 16, kTn = WC * 64, kBuf = (kTm + kTn) * kStageRowBytes;
+    constexpr int kCopyA = kTm / 8 / kWaves, kCopyB = kTn / 8 / kWaves;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S * kBuf];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int z = blockIdx.x % g.splits;
     int b, ti, tj;
-    if (!tile_at<KIND>(g, blockIdx.x / g.splits, b, ti, tj)) return;
-    const int i0 = ti * T, j0 = tj * T;
-    const HalfSrc<SPLIT> src(g, b, i0, j0, T);
-    const int s0 = z * g.per, s1 = min(src.total, s0 + g.per);
-    auto copy = [&](int s) {
-        uint8_t *buf = lds + (s & 1) * kBuf;
-        const auto rp = src.a(s), rq = src.b(s);
-        const int kb = src.k(s);
+    if (!tile_at<KIND>(g, blockIdx.x / g.splits, g.mt, g.nt, g.tiles, b, ti, tj)) return;
+    const int i0 = ti * kTm, j0 = tj * kTn;
+    const HalfSrc<SPLIT> src(g, b, i0, j0, kTm, kTn, z);
+    auto copy = [&](int s, uint8_t *buf) {
+        const int at_a = src.at_a(s), at_b = src.at_b(s);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            copy_rows<0>(rp, buf + (wave * 4 + q) * 1024, lane, wave * 4 + q, src.ld_a, kb, kStageRowBytes);
-            copy_rows<2>(rq, buf + T * kStageRowBytes + (wave * 4 + q) * 1024, lane, wave * 4 + q, src.ld_b, kb,
-                         kStageRowBytes);
+        for (int c = 0; c < kCopyA; ++c) {
+            const int q = wave * kCopyA + c;
+            copy_rows<0>(src.rp, buf + q * 1024, lane, q, src.ld_a, at_a, kStageRowBytes);
+        }
+#pragma unroll
+        for (int c = 0; c < kCopyB; ++c) {
+            const int q = wave * kCopyB + c;
+            copy_rows<2>(src.rq, buf + kTm * kStageRowBytes + q * 1024, lane, q, src.ld_b, at_b, kStageRowBytes);
         }
     };
-    const int wi = (wave >> 1) * 64, wj = (wave & 1) * 64, q = lane & 15;
-    v4f acc[4][4];
+    const int wi = wave / WC * (M * 16), wj = wave % WC * 64, q = lane & 15;
+    v4f acc[M][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < M; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = v4f{0, 0, 0, 0};
-    if (s0 < s1) copy(s0);
-    for (int s = s0; s < s1; ++s) {
-        wait_vmem<0>();
+#pragma unroll
+    for (int u = 0; u < S - 1; ++u)
+        if (u < src.total) copy(u, lds + u * kBuf);
+    int u = 0;   // s % S
+    for (int s = 0; s < src.total; ++s) {
+        // this stage has landed; those after it, if there are S - 2, need not
+        if (S > 2 && s + S - 1 <= src.total) wait_vmem<(S - 2) * (kCopyA + kCopyB)>();
+        else wait_vmem<0>();
         lds_barrier();
-        const uint8_t *buf = lds + (s & 1) * kBuf;
-        if (s + 1 < s1) copy(s + 1);
-        v8i fa[4], fb[4];
+        const uint8_t *buf = lds + u * kBuf;
+        if (s + S - 1 < src.total) copy(s + S - 1, lds + (u == 0 ? S - 1 : u - 1) * kBuf);
+        v8i fb[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            fa[i] = read_fragment<0>(buf, wi + 16 * i + q, lane);
-            fb[i] = read_fragment<2>(buf + T * kStageRowBytes, wj + 4 * q + i, lane);
-        }
+        for (int j = 0; j < 4; ++j) fb[j] = read_fragment<2>(buf + kTm * kStageRowBytes, wj + 4 * q + j, lane);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int i = 0; i < M; ++i) {
+            const v8i fa = read_fragment<0>(buf, wi + 16 * i + q, lane);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const v4i x = h ? fa[i].hi : fa[i].lo, y = h ? fb[j].hi : fb[j].lo;
+                    const v4i x = h ? fa.hi : fa.lo, y = h ? fb[j].hi : fb[j].lo;
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8f16, x),
                                                                        __builtin_bit_cast(v8f16, y), acc[i][j], 0, 0, 0);
                 }
-    }
-    float *out = g.parts + ((int64_t)z * g.batch + b) * g.rows * g.cols;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = i0 + wi + 16 * i + 4 * (lane >> 4) + e, col = j0 + wj + 4 * q;
-            *reinterpret_cast<v4f *>(out + (int64_t)row * g.cols + col) = v4f{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
         }
+        u = u + 1 == S ? 0 : u + 1;
+    }
+    const bool whole = g.splits == 1;
+    const bool rows = !whole || writes_rows<KIND>(g), across = whole && writes_across<KIND>(g, ti, tj);
+    float *part = part_of(g, z, b);
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        const int row = i0 + wi + 16 * i + 4 * (lane >> 4), col = j0 + wj + 4 * q;
+        if (rows)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const v4f v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+                if (whole) emit<SPLIT, KIND, false, 4>(g, b, row + e, col, v);
+                else if (row + e < g.rows && col < g.cols)
+                    *reinterpret_cast<v4f *>(part + (int64_t)(row + e) * g.cols + col) = v;
+            }
+        if (across)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) emit<SPLIT, KIND, true, 4>(g, b, row, col + j, acc[i][j]);
+    }
 }
 
 // Adds up the splits in their order and writes D and its transpose, 64 x 64 per
-// workgroup, a quarter of a tile of product_parts.
+// workgroup.
 template <bool SPLIT, Product KIND>
 __global__ __launch_bounds__(256) void product_join(ProductArgs g) {
     __shared__ float tile[64][65];
-    const int tid = threadIdx.x, quarter = blockIdx.x & 3;
+    const int tid = threadIdx.x, mt = g.rows / 64, nt = g.cols / 64;
     int b, ti, tj;
-    if (!tile_at<KIND>(g, blockIdx.x >> 2, b, ti, tj)) return;
-    const int i0 = ti * kPad + (quarter >> 1) * 64, j0 = tj * kPad + (quarter & 1) * 64;
-    const bool rows = KIND != kLast || g.o_col == 1;
-    const bool across = symmetric(KIND) ? ti != tj : KIND != kLast || !rows;
-    const int64_t plane = (int64_t)g.rows * g.cols;
+    if (!tile_at<KIND>(g, blockIdx.x, mt, nt, symmetric(KIND) ? mt * (mt + 1) / 2 : mt * nt, b, ti, tj)) return;
+    const int i0 = ti * 64, j0 = tj * 64;
+    const bool rows = writes_rows<KIND>(g), across = writes_across<KIND>(g, ti, tj);
+    const int64_t plane = (int64_t)g.batch * g.rows * g.cols;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int row = 32 * h + (tid >> 3), col = (tid & 7) * 8;
-        const float *at = g.parts + b * plane + (int64_t)(i0 + row) * g.cols + j0 + col;
+        const float *at = part_of(g, 0, b) + (int64_t)(i0 + row) * g.cols + j0 + col;
         v4f lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
         for (int z = 0; z < g.splits; ++z) {
-            lo += *reinterpret_cast<const v4f *>(at + z * g.batch * plane);
-            hi += *reinterpret_cast<const v4f *>(at + z * g.batch * plane + 4);
+            lo += *reinterpret_cast<const v4f *>(at + z * plane);
+            hi += *reinterpret_cast<const v4f *>(at + z * plane + 4);
         }
         const v8f v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        if (rows) emit<SPLIT, KIND, false>(g, b, i0 + row, j0 + col, v);
+        if (rows) emit<SPLIT, KIND, false, 8>(g, b, i0 + row, j0 + col, v);
         if (across)
 #pragma unroll
             for (int j = 0; j < 8; ++j) tile[row][col + j] = v[j];
@@ -404,7 +476,7 @@ __global__ __launch_bounds__(256) void product_join(ProductArgs g) {
         v8f v;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = tile[row + i][col];
-        emit<SPLIT, KIND, true>(g, b, i0 + row, j0 + col, v);
+        emit<SPLIT, KIND, true, 8>(g, b, i0 + row, j0 + col, v);
     }
 }
 
@@ -429,30 +501,48 @@ struct Buffers {
 
 // How a product of rows x cols (padded) and `stages` stages is launched.
 struct ProductPlan {
-    bool pipe;
+    int size;            // tile rows and columns: 256 (the pipeline), 128 or 64
     int mt, nt, tiles;   // per matrix
     int splits, per;
 };
-// 256 x 256 tiles from half a tile per CU on: they take twice as long as four of 128
-// x 128 on a CU of their own, but feed the MFMA pipe 1.5 times as well.  Smaller
-// tiles are split until two for each CU are in flight, from 4 stages each.
+// The time of a launch is estimated (us) from its workgroups W and the stages n of
+// each: W / 512 rounds of two workgroups per CU (the pipeline: W / 256 of one),
+// `pair` a stage with both in place and `one` with one, then the writing, or, of a
+// split launch, the sums' way through memory and the joining.  Measured, and the
+// estimate's choice within 10% of the best of 18 launches each:
+//   r = c = 2048, one part, A: 64 28 us, 128 25, 128 in 2 splits 24, 256 50
+//   r = c = 4096, one part, A: 128 102, 256 96;  two parts: 128 321, in 2 splits 265
+//   r = c = 1024, two parts, A: 64 21, 128 in 4 splits 20, 256 96
+//   300 x 900, two parts, A: 64 20, in 4 splits 12, 128 in 4 splits 17
 ProductPlan plan_product(int batch, int rows, int cols, int stages, bool sym) {
-    auto count = [&](int q, int &mt, int &nt) {
-        mt = (int)ceil_div(rows, q);
-        nt = (int)ceil_div(cols, q);
-        return sym ? mt * (mt + 1) / 2 : mt * nt;
+    struct Size {
+        int size, resident;
+        double fixed, one, pair;
     };
-    ProductPlan p;
-    p.tiles = count(kPipeTile, p.mt, p.nt);
-    p.pipe = (int64_t)p.tiles * batch >= kCus / 2;
-    p.splits = 1;
-    p.per = stages;
-    if (p.pipe) return p;
-    p.tiles = count(kPad, p.mt, p.nt);
-    const int64_t want = std::min<int64_t>(ceil_div(2 * kCus, (int64_t)p.tiles * batch), std::max(1, stages / 4));
-    p.per = (int)ceil_div(stages, want);
-    p.splits = (int)ceil_div(stages, p.per);
-    return p;
+    constexpr Size sizes[] = {{64, 2, 2.5, 0.42, 0.60}, {128, 2, 3.0, 0.68, 1.06}, {kPipeTile, 1, 6.0, 1.40, 1.40}};
+    const double entries = (double)batch * rows * cols * (sym ? 0.5 : 1.0);
+    ProductPlan best = {};
+    double least = 0.0;
+    for (const Size &s : sizes)
+        for (int want = 1; want <= 16; want *= 2) {
+            ProductPlan p;
+            p.size = s.size;
+            p.mt = (int)ceil_div(rows, s.size);
+            p.nt = (int)ceil_div(cols, s.size);
+            p.tiles = sym ? p.mt * (p.mt + 1) / 2 : p.mt * p.nt;
+            p.per = (int)ceil_div(stages, want);
+            p.splits = (int)ceil_div(stages, p.per);
+            if (want > 1 && p.per < 4) break;
+            const int64_t groups = (int64_t)p.tiles * batch * p.splits, round = (int64_t)kCus * s.resident, rest = groups % round;
+            double t = s.fixed + p.per * (groups / round * s.pair + (rest > kCus ? s.pair : rest > 0 ? s.one : 0.0));
+            t += entries * 2e-6;
+            if (p.splits > 1) t += 3.0 + 0.6 * p.splits + p.splits * entries * 0.8e-6;
+            if (best.tiles == 0 || t < least) {
+                least = t;
+                best = p;
+            }
+        }
+    return best;
 }
 
 // One part per held matrix for bf16, two otherwise.
@@ -470,10 +560,9 @@ size_t carve(int batch, int r, int c, bool split, void *base, Buffers *out) {
     auto planes = [&](int64_t rows, int64_t cols) {
         Planes m;
         m.pitch = cols;
-        m.batch = rows * cols;
-        const size_t bytes = sizeof(f16) * (size_t)m.batch * batch;
-        m.hi = reinterpret_cast<f16 *>(take(bytes));
-        m.lo = split ? reinterpret_cast<f16 *>(take(bytes)) : nullptr;
+        m.lo = split ? rows * cols : 0;
+        m.batch = rows * cols + m.lo;
+        m.hi = reinterpret_cast<f16 *>(take(sizeof(f16) * (size_t)m.batch * batch));
         return m;
     };
     Buffers b;
@@ -488,7 +577,7 @@ size_t carve(int batch, int r, int c, bool split, void *base, Buffers *out) {
     const int passes = split ? 3 : 1;
     auto room = [&](int64_t rows, int64_t cols, int64_t k, bool sym) {
         const ProductPlan p = plan_product(batch, (int)rows, (int)cols, passes * (int)(k / 64), sym);
-        if (!p.pipe) sums = std::max(sums, p.splits * rows * cols);
+        if (p.splits > 1) sums = std::max(sums, p.splits * rows * cols);
     };
     room(rp, rp, cp, true);
     room(rp, rp, rp, true);
@@ -508,13 +597,19 @@ void launch_product(ProductArgs &g, int batch, hipStream_t st) {
     g.batch = batch;
     g.splits = p.splits;
     g.per = p.per;
-    const int64_t all = (int64_t)p.tiles * batch;
-    if (p.pipe) {
+    const int64_t all = (int64_t)p.tiles * batch * p.splits;
+    if (p.size == kPipeTile) {
         g.chunk = (int)ceil_div(all, kXcds);
         product_pipe<SPLIT, KIND><<<(unsigned)(kXcds * g.chunk), 256, 0, st>>>(g);
+    } else if (p.size == 128) {
+        product_tile<SPLIT, KIND, 2, 2, 4, 2><<<(unsigned)all, 256, 0, st>>>(g);
     } else {
-        product_parts<SPLIT, KIND><<<(unsigned)(all * p.splits), 256, 0, st>>>(g);
-        product_join<SPLIT, KIND><<<(unsigned)(all * 4), 256, 0, st>>>(g);
+        product_tile<SPLIT, KIND, 4, 1, 1, 4><<<(unsigned)all, 256, 0, st>>>(g);
+    }
+    if (p.splits > 1) {
+        const int mt = g.rows / 64, nt = g.cols / 64;
+        const int64_t blocks = (symmetric(KIND) ? (int64_t)mt * (mt + 1) / 2 : (int64_t)mt * nt) * batch;
+        product_join<SPLIT, KIND><<<(unsigned)blocks, 256, 0, st>>>(g);
     }
 }
 
@@ -523,10 +618,12 @@ hipError_t run_ortho(const OrthoArgs &o, const Buffers &b, hipStream_t st) {
     const int r = o.rows, c = o.cols;
     const int rt = (int)ceil_div(r, kPad), ct = (int)ceil_div(c, kPad);
     const bool along_c = o.g_col == 1;
-    norm_parts<<<dim3(kParts, o.batch), 256, 0, st>>>(
-        {o.G, along_c ? o.g_row : o.g_col, o.g_batch, along_c ? r : c, along_c ? c : r, o.type, b.parts});
-    PrepArgs p = {o.G, o.g_row, o.g_col, o.g_batch, r, c, o.type, b.parts, o.eps, ldexp(1.0, kScaleX), b.x, b.t[0], ct * 2};
-    prepare_x<SPLIT><<<dim3(rt * 2 * ct * 2, o.batch), 256, 0, st>>>(p);
+    const Lines lines = {o.G, along_c ? o.g_row : o.g_col, o.g_batch, along_c ? r : c, along_c ? c : r, o.type};
+    const int count = (int)std::min<int64_t>(kParts, ceil_div((int64_t)r * c, 4096));
+    norm_parts<<<dim3(count, o.batch), 256, 0, st>>>(lines, count, b.parts);
+    const PrepArgs p = {lines, b.parts, count, o.eps, ldexp(1.0, kScaleX), along_c ? b.x : b.t[0], along_c ? b.t[0] : b.x,
+                        along_c ? ct : rt};
+    prepare_x<SPLIT><<<dim3(rt * ct, o.batch), 256, 0, st>>>(p);
     ProductArgs g = {};
     g.O = o.O;
     g.o_row = o.o_row;
@@ -551,18 +648,18 @@ hipError_t run_ortho(const OrthoArgs &o, const Buffers &b, hipStream_t st) {
         g.kblocks = cp / 64;
         g.mul = (float)ldexp(1.0, kScaleA - 2 * kScaleX);
         launch_product<SPLIT, kGram>(g, o.batch, st);
-        g.p = g.q = g.e = g.et = b.a;
+        g.p = g.q = g.e = b.a;
         g.d = g.dt = b.b;
         g.kblocks = rp / 64;
+        g.diag = (float)ldexp(k[0], kScaleB);
         g.add = (float)ldexp(k[1], kScaleB - kScaleA);
         g.mul = (float)ldexp(k[2], kScaleB - 2 * kScaleA);
         launch_product<SPLIT, kPoly>(g, o.batch, st);
         g.p = b.b;
-        g.q = g.et = t;
-        g.e = g.d = b.x;
+        g.q = t;
+        g.d = b.x;
         g.dt = t_next;
         g.cols = cp;
-        g.add = (float)k[0];
         g.mul = (float)ldexp(1.0, -kScaleB);
         if (step + 1 < o.steps) launch_product<SPLIT, kUpdate>(g, o.batch, st);
         else launch_product<SPLIT, kLast>(g, o.batch, st);

@@ -75,14 +75,14 @@ __device__ inline PipeWave pipe_wave(uint8_t *lds) {
     return w;
 }
 
-// Copy t (0..3) of half h of an operand's stage: 64 t + 4 h rows on.  `left`: the
-// operand's bytes from this stage on; none are read past them (left <= 0: zeros).
-__device__ inline void pipe_copy(const PipeWave &w, __amdgpu_buffer_rsrc_t r, int ld, int stage, int left, uint8_t *dst,
+// Copy t (0..3) of half h of an operand's stage, which lies `at` bytes from the
+// descriptor's start: 64 t + 4 h rows on.  `left`: the operand's bytes from there on; none are read past them (left <= 0: zeros).
+__device__ inline void pipe_copy(const PipeWave &w, __amdgpu_buffer_rsrc_t r, int ld, int at, int left, uint8_t *dst,
                                  int h, int t) {
     int off = (w.copy_row + 64 * t + 4 * h) * ld + w.chunk16;
     if (left < kStageRowBytes) off = w.chunk16 < left ? off : 0x7FFFFFF0;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr *)(dst + h * kHalfBytes + (4 * t + w.wave) * 1024), 16, off,
-                                             left > 0 ? stage * kStageRowBytes : 0, 0, 0);
+                                             left > 0 ? at : 0, 0, 0);
 }
 
 // Fragment i of the strip at `at`: 32 bytes a lane.
@@ -113,8 +113,8 @@ __device__ inline void pipe_zero(v4f (&acc)[8][8]) {
 }
 
 // The product of `stages` stages into acc, which is zeroed here.  Src gives the
-// operands of a stage: a(s), b(s) descriptors, k(s) the stage within them, left(s)
-// the bytes from there on (<= 0 for s >= stages), ld_a, ld_b; Op the arithmetic:
+// operands of a stage: a(s), b(s) descriptors, at_a(s), at_b(s) its place in them,
+// left(s) the bytes from there on (<= 0 for s >= stages), ld_a, ld_b; Op the arithmetic:
 // fetch(s) asks for what stage s needs besides (it may issue any number of
 // loads), begin(s) takes it into use, mma<i, j, p>(acc[i][j], a, b) multiplies, in
 // kParts MFMAs of 8 blocks' distance to each other, and mask(f, s) clears what the last stage's fragments hold past the rows' ends.
@@ -129,10 +129,10 @@ __device__ inline void pipe_run(const PipeWave &w, Op &op, const Src &src, int s
     constexpr int P = Op::kParts;
     auto buffer = [&](int s) { return w.lds + (s & 1) * kPipeStage; };
     auto copy_a = [&](int s, int h, int t) {
-        pipe_copy(w, src.a(s), src.ld_a, src.k(s), src.left(s), buffer(s), h, t);
+        pipe_copy(w, src.a(s), src.ld_a, src.at_a(s), src.left(s), buffer(s), h, t);
     };
     auto copy_b = [&](int s, int c) {
-        pipe_copy(w, src.b(s), src.ld_b, src.k(s), src.left(s), buffer(s) + kOperandBytes, c >> 2, c & 3);
+        pipe_copy(w, src.b(s), src.ld_b, src.at_b(s), src.left(s), buffer(s) + kOperandBytes, c >> 2, c & 3);
     };
     op.fetch(0);   // before the copies, so that its wait is none of theirs
 #pragma unroll

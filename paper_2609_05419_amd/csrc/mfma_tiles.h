@@ -46,15 +46,15 @@ __device__ inline __amdgpu_buffer_rsrc_t rows_of(const uint8_t *base, int rows, 
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), (short)0, extent, 0x00020000);
 }
 
-// Copy rows [8 q, 8 q + 8) of stage kb to dst (wave-uniform, 1 KB).  `left` is
-// the operand's bytes from this stage on: chunks past it are read as zeros.  S:
+// Copy rows [8 q, 8 q + 8) of a stage, which lies `at` bytes from the descriptor's
+// start, to dst (wave-uniform, 1 KB).  `left` is the operand's bytes from there on: chunks past it are read as zeros.  S:
 // the chunk c of row r lies in slot c ^ (r >> S & 7).
 template <int S>
-__device__ inline void copy_rows(__amdgpu_buffer_rsrc_t r, uint8_t *dst, int lane, int q, int ld, int kb, int left) {
+__device__ inline void copy_rows(__amdgpu_buffer_rsrc_t r, uint8_t *dst, int lane, int q, int ld, int at, int left) {
     const int row = 8 * q + (lane >> 3), chunk16 = ((lane & 7) ^ (row >> S & 7)) << 4;
     int off = row * ld + chunk16;
     if (left < kStageRowBytes) off = chunk16 < left ? off : 0x7FFFFFF0;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr *)dst, 16, off, kb * kStageRowBytes, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr *)dst, 16, off, at, 0, 0);
 }
 
 // Zero the bytes of row `row` past `left` in the chunk that holds byte `left`.

@@ -131,7 +131,7 @@ def orthogonalize_bound(sigma, cols, parts, dtype, steps=5, coef=COEF):
     the matrix with the singular values p(s) = a s + b s^3 + c s^5 and the same
     singular vectors, so an error of X comes out multiplied by at most max |p'| over
     [0, s_max].  A step adds the roundings of what it holds, u relative in each
-    entry of A, B and X (u: half a step of fp16, or its square for two parts,
+    entry of A, B = a + b A + c A^2 and X (u: half a step of fp16, or its square for two parts,
     once more for the left-out product of the low parts; and 2 (n + 2) 2^-23 for
     the fp32 sums of n terms, in the norm of the factors): those of A go into B
     through b + 2 c A, those of B into X through X."""
@@ -149,7 +149,7 @@ def orthogonalize_bound(sigma, cols, parts, dtype, steps=5, coef=COEF):
         gain = np.abs(a + 3 * b * grid ** 2 + 5 * c * grid ** 4).max()
         fp = 2.0 ** -23
         d_a = u * frob(s2) + 2 * (cols + 2) * fp * frob(s) ** 2
-        held_b = b * s2 + c * s2 ** 2
+        held_b = a + b * s2 + c * s2 ** 2
         d_b = (abs(b) + 2 * abs(c) * top ** 2) * d_a + u * frob(held_b) + 2 * (r + 2) * fp * abs(c) * frob(s2) ** 2
         d_x = top * d_b + u * frob(sigma[t + 1]) + 2 * (r + 2) * fp * frob(held_b) * frob(s)
         err = gain * err + d_x
