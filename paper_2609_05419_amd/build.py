@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libo2m.so")
 SOURCES = ["api.hip", "k_scale.hip", "k_residue.hip", "k_gemm.hip", "k_crt.hip", "moduli.cpp",
            "api_model.hip", "k_quant.hip", "k_fp8.hip", "k_fp8_scaled.hip", "k_fp8_partial.hip", "k_fp8_wide.hip",
-           "k_fp8_few.hip", "k_ortho.hip"]
+           "k_fp8_few.hip", "k_ortho.hip", "k_ortho_small.hip"]
 # measurement probes (the practical int8 MFMA ceiling, HBM streaming rates), a
 # library of their own
 PROBE_LIB = os.path.join(HERE, "libo2m_probe.so")

@@ -27,26 +27,16 @@
 //
 // Bound: fp16 MFMA; 1.5 r^2 c + 0.5 r^3 multiply-adds a step, halves counted once, and
 // three times that for two parts.
-#include "fp8_round.h"
-#include "mfma_pipe.h"
-#include "mfma_tiles.h"
-#include "model_internal.h"
+#include "ortho_shared.h"
 #include "tile_schedule.h"
 
 #include <algorithm>
-#include <hip/hip_bf16.h>
-#include <hip/hip_fp16.h>
 #include <math.h>
 
 namespace o2m {
 namespace {
 
-typedef _Float16 f16;
-typedef f16 v8f16 __attribute__((ext_vector_type(8)));
-typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
-
 constexpr int kPad = 64;
-constexpr int kScaleX = 14, kScaleA = 11, kScaleB = 6;
 constexpr int kParts = 1024;   // partial sums of the norm, at most, per matrix
 
 struct Planes {
@@ -55,12 +45,6 @@ struct Planes {
     int64_t pitch;    // elements of a row
     int64_t batch;    // from matrix to matrix, both parts
 };
-
-__device__ inline void store_any(void *p, int64_t i, int type, float v) {
-    if (type == O2M_TYPE_F32) static_cast<float *>(p)[i] = v;
-    else if (type == O2M_TYPE_F16) static_cast<__half *>(p)[i] = __float2half(v);
-    else static_cast<__hip_bfloat16 *>(p)[i] = __float2bfloat16(v);
-}
 
 // An entry held in one or two parts.
 template <bool SPLIT>
@@ -82,22 +66,6 @@ __device__ inline void hold_run(const Planes &m, int64_t i, const V &v) {
     *reinterpret_cast<vf16 *>(m.hi + i) = hi;
     if (SPLIT) *reinterpret_cast<vf16 *>(m.hi + m.lo + i) = __builtin_convertvector(v - __builtin_convertvector(hi, V), vf16);
 }
-// Eight neighbouring entries, of which the first n exist, zeros after them.
-__device__ inline v8f load_some(const void *p, int64_t i, int n, int type) {
-    float v[8];
-    if (type == O2M_TYPE_F32) load8(static_cast<const float *>(p) + i, n, v);
-    else if (type == O2M_TYPE_F16) load8(static_cast<const __half *>(p) + i, n, v);
-    else load8(static_cast<const __hip_bfloat16 *>(p) + i, n, v);
-    return v8f{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-}
-
-// G of a batch as lines of contiguous entries.
-struct Lines {
-    const void *G;
-    int64_t line, batch;   // strides
-    int lines, len, type;
-};
-
 // Sums of squares in fp64: part z adds up the runs of 8 entries z, z + parts, ..,
 // its threads in a fixed order, so that every run of the call adds in the same one.
 __global__ __launch_bounds__(256) void norm_parts(Lines g, int parts, double *out) {
@@ -676,6 +644,7 @@ size_t ortho_workspace(int batch, int rows, int cols, int type) {
 hipError_t launch_ortho(const OrthoArgs &o, void *ws, hipStream_t st) {
     Buffers b;
     const bool split = split_of(o.type);
+    if (ortho_is_small(o.rows, o.cols, split, o.steps)) return launch_ortho_small(o, split, st);
     carve(o.batch, o.rows, o.cols, split, ws, &b);
     return split ? run_ortho<true>(o, b, st) : run_ortho<false>(o, b, st);
 }

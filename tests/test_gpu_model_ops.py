@@ -295,7 +295,7 @@ def check_orthogonalize(got, g, dtype, steps=5, coef=R.COEF, eps=1e-7):
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 200), (96, 80), (64, 64), (128, 128), (130, 129), (33, 500), (300, 256),
-                                       (257, 900)])
+                                       (257, 900), (17, 250), (127, 33), (64, 256), (90, 101), (112, 112), (513, 700)])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("order", ["row", "col"])
 def test_orthogonalize(o2m, rows, cols, dtype, order):
