@@ -38,119 +38,150 @@ __device__ inline void store_bytes(uint8_t *p, uint2 w, int n) {
     }
 }
 
-// One tile of 128 x 128 entries per workgroup, quantized along its lines, across
-// them or both.  Thread (rg, cg) holds the 8 x 8 entries of lines 8 rg.. and
-// positions 8 cg..: 16 threads share a line, whose maximum is taken by lane
-// exchanges, and the maxima across lines and the bytes of the transposed operand
-// go through LDS (in 8-byte units of 8 lines, unit rg of position q in slot rg ^
-// (q / 8), which spreads both the writes and the reads over the banks).
+// The largest finite magnitude of eight entries, as bits.
 template <class T>
-__global__ __launch_bounds__(256) void quantize_tile(QuantArgs g) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[128 * 128];
-    __shared__ float tile_max[4];
-    const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
-    const int tp = blockIdx.x / g.tiles_q, tq = blockIdx.x % g.tiles_q;
-    const int p0 = tp * 128 + 8 * rg, q0 = tq * 128 + 8 * cg;
-    const int nq = min(8, g.len - q0);
-    float x[8][8], row_max[8], col_max[8];
+__device__ inline uint32_t largest_finite_of(const Run8<T> &r) {
+    uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) col_max[j] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        load8<T>(static_cast<const T *>(g.X) + (int64_t)(p0 + i) * g.ld + q0, p0 + i < g.lines ? nq : 0, x[i]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float m = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float a = magnitude(x[i][j]);
-            m = fmaxf(m, a);
-            col_max[j] = fmaxf(col_max[j], a);
-        }
-#pragma unroll
-        for (int s = 1; s < 16; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
-        row_max[i] = m;
+    for (int i = 0; i < Run8<T>::kWords; ++i) {
+        const uint32_t w = magnitude_bits<T>(r.w[i]), lo = Run8<T>::kHalves ? w & 0xFFFFu : w, hi = Run8<T>::kHalves ? w >> 16 : 0;
+        m = max(m, max(bits_finite<T>(lo) ? lo : 0u, bits_finite<T>(hi) ? hi : 0u));
     }
-    const bool whole = g.along.block == kBlockK || g.across.block == kBlockK;
-    float all = 0.0f;
-    if (whole) {   // (uniform over the workgroup)
+    return m;
+}
+// Words with Inf and NaN replaced by zeros.
+template <class T>
+__device__ inline uint32_t finite_word(uint32_t w) {
+    w = magnitude_bits<T>(w);
+    if (!Run8<T>::kHalves) return bits_finite<T>(w) ? w : 0u;
+    return (bits_finite<T>(w & 0xFFFFu) ? w & 0xFFFFu : 0u) | (bits_finite<T>(w >> 16) ? w & 0xFFFF0000u : 0u);
+}
+
+// One tile of 128 x 128 entries per workgroup, quantized along its lines, across
+// them or both.  Thread (rg, cg) holds the 4 x 8 entries of lines 4 rg .. and
+// positions 8 cg ..: 16 lanes share a line, whose maximum is taken by lane
+// exchanges; the maxima across lines go through LDS, and so do the bytes of the
+// transposed operand, in words of 4 lines: word rg of position q lies at rg ^ 2 (q /
+// 8), which spreads both the writes and the reads over the banks.
+//
+// Bound: memory; the vector unit comes next, which is why maxima are taken on the
+// bits as they come and Inf and NaN are looked for once a tile.
+constexpr int kTileThreads = 512;
+template <class T, bool ALONG, bool ACROSS>
+__global__ __launch_bounds__(kTileThreads, 4) void quantize_tile(QuantArgs g) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[ACROSS ? 128 * 128 : 16];
+    __shared__ uint32_t part[ACROSS ? 8 : 1][ACROSS ? 128 : 1];   // maxima of each wave's lines
+    __shared__ uint32_t wave_max[8];
+    constexpr int W = Run8<T>::kWords;
+    const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4, wave = tid >> 6;
+    const int tp = blockIdx.x / g.tiles_q, tq = blockIdx.x % g.tiles_q;
+    const int p0 = tp * 128 + 4 * rg, q0 = tq * 128 + 8 * cg;
+    const int nq = min(8, g.len - q0);
+    Run8<T> x[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) all = fmaxf(all, row_max[i]);
-        all = fmaxf(all, __shfl_xor(all, 16));
-        all = fmaxf(all, __shfl_xor(all, 32));
-        if ((tid & 63) == 0) tile_max[tid >> 6] = all;
+    for (int i = 0; i < 4; ++i)
+        x[i] = load_run(static_cast<const T *>(g.X) + (int64_t)(p0 + i) * g.ld + q0, p0 + i < g.lines ? nq : 0);
+
+    uint32_t row_max[4], all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        row_max[i] = largest_of(x[i]);
+        all = max(all, row_max[i]);
+    }
+    const bool fine = !__syncthreads_or(!bits_finite<T>(all));
+    if (!fine) {
+        all = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            row_max[i] = largest_finite_of(x[i]);
+            all = max(all, row_max[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) row_max[i] = largest_of_16(row_max[i]);
+    const bool whole = (ALONG && g.along.block == kBlockK) || (ACROSS && g.across.block == kBlockK);
+    if (whole) {   // (uniform over the workgroup)
+        all = larger_of_rows<float>(largest_of_16(all));
+        if ((tid & 63) == 0) wave_max[wave] = all;
         __syncthreads();
-        all = fmaxf(fmaxf(tile_max[0], tile_max[1]), fmaxf(tile_max[2], tile_max[3]));
+#pragma unroll
+        for (int w = 0; w < 8; ++w) all = max(all, wave_max[w]);
     }
 
-    if (g.along.values) {
+    if (ALONG) {
         const Dest &d = g.along;
-        const float top = d.format == O2M_FP8_E4M3 ? 448.0f : 57344.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const Scale s = scale_of(d.block == 1 ? row_max[i] : all, d.format, d.scale_type);
+        for (int i = 0; i < 4; ++i) {
+            const Scale s = scale_of(bits_value<T>(d.block == 1 ? row_max[i] : all), d.format, d.scale_type);
             if (p0 + i >= g.lines || nq <= 0) continue;
-            float y[4], z[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                y[j] = scaled(x[i][j], s.inv, top);
-                z[j] = scaled(x[i][4 + j], s.inv, top);
-            }
-            store_bytes(d.values + (int64_t)(p0 + i) * d.ld + q0, uint2{pack_fp8(y, d.format), pack_fp8(z, d.format)}, nq);
+            const uint2 w = fine ? round_run<true>(x[i], s.inv, d.format) : round_run<false>(x[i], s.inv, d.format);
+            store_bytes(d.values + (int64_t)(p0 + i) * d.ld + q0, w, nq);
             if (cg == 0 && d.block == 1) store_scale(d, p0 + i, tq, s.held);
             if (tid == 0 && i == 0 && d.block == kBlockK) store_scale(d, tp, tq, s.held);
         }
     }
 
-    if (g.across.values) {
+    if (ACROSS) {
         const Dest &d = g.across;
-        const float top = d.format == O2M_FP8_E4M3 ? 448.0f : 57344.0f;
-        Scale s[8];
+        float inv[8];
         if (d.block == 1) {
-            float *part = reinterpret_cast<float *>(lds);   // [16][128]
 #pragma unroll
-            for (int j = 0; j < 8; ++j) part[rg * 128 + 8 * cg + j] = col_max[j];
-            __syncthreads();
-            float m = 0.0f;
-            if (tid < 128) {
-                for (int r = 0; r < 16; ++r) m = fmaxf(m, part[r * 128 + tid]);
+            for (int i = 0; i < W; ++i) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int l = 0; l < 4; ++l) m = larger<T>(m, fine ? magnitude_bits<T>(x[l].w[i]) : finite_word<T>(x[l].w[i]));
+                m = larger_of_rows<T>(m);
+                if ((tid & 63) < 16) {
+                    if (Run8<T>::kHalves) {
+                        part[wave][8 * cg + 2 * i] = m & 0xFFFFu;
+                        part[wave][8 * cg + 2 * i + 1] = m >> 16;
+                    } else {
+                        part[wave][8 * cg + i] = m;
+                    }
+                }
             }
             __syncthreads();
-            if (tid < 128) part[tid] = m;
+            if (tid < 128) {   // a position each: its scale, and the inverse for the others
+                uint32_t m = 0;
+#pragma unroll
+                for (int w = 0; w < 8; ++w) m = max(m, part[w][tid]);
+                const Scale s = scale_of(bits_value<T>(m), d.format, d.scale_type);
+                part[0][tid] = __float_as_uint(s.inv);   // (only this thread reads this column)
+                if (tq * 128 + tid < g.len) store_scale(d, tq * 128 + tid, tp, s.held);
+            }
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                s[j] = scale_of(part[8 * cg + j], d.format, d.scale_type);
-                if (rg == 0 && j < nq) store_scale(d, q0 + j, tp, s[j].held);
-            }
-            __syncthreads();   // before the bytes overwrite the maxima
+            for (int j = 0; j < 8; ++j) inv[j] = __uint_as_float(part[0][8 * cg + j]);
         } else {
-            const Scale t = scale_of(all, d.format, d.scale_type);
+            const Scale s = scale_of(bits_value<T>(all), d.format, d.scale_type);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] = t;
-            if (tid == 0) store_scale(d, tq, tp, t.held);
+            for (int j = 0; j < 8; ++j) inv[j] = s.inv;
+            if (tid == 0) store_scale(d, tq, tp, s.held);
         }
+        const float top = d.format == O2M_FP8_E4M3 ? 448.0f : 57344.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float y[4], z[4];
+            float y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                y[i] = scaled(x[i][j], s[j].inv, top);
-                z[i] = scaled(x[4 + i][j], s[j].inv, top);
-            }
-            *reinterpret_cast<uint2 *>(lds + (8 * cg + j) * 128 + ((rg ^ cg) << 3)) =
-                uint2{pack_fp8(y, d.format), pack_fp8(z, d.format)};
+            for (int i = 0; i < 4; ++i) y[i] = fine ? entry(x[i], j) * inv[j] : scaled(entry(x[i], j), inv[j], top);
+            *reinterpret_cast<uint32_t *>(lds + (8 * cg + j) * 128 + ((rg ^ (2 * cg)) << 2)) = pack_fp8(y, d.format);
         }
         __syncthreads();
-        // unit u (8 lines) of position q: 16 consecutive threads write the 128
-        // bytes of one operand row
+        // 8 consecutive threads write the 128 bytes of one operand row
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int q = 16 * i + (tid >> 4), u = tid & 15;
-            const uint2 w = *reinterpret_cast<const uint2 *>(lds + q * 128 + ((u ^ (q >> 3)) << 3));
-            const int line = tp * 128 + 8 * u;
-            if (tq * 128 + q < g.len && line < g.lines)
-                store_bytes(d.values + (int64_t)(tq * 128 + q) * d.ld + line, w, min(8, g.lines - line));
+        for (int i = 0; i < 2; ++i) {
+            const int q = 64 * i + (tid >> 3), u = tid & 7, turn = q >> 3;   // bytes 16 u ..: words 4 u ..
+            const uint2 lo = *reinterpret_cast<const uint2 *>(lds + q * 128 + (((2 * u) ^ turn) << 3));
+            const uint2 hi = *reinterpret_cast<const uint2 *>(lds + q * 128 + (((2 * u + 1) ^ turn) << 3));
+            const int line = tp * 128 + 16 * u, n = g.lines - line;
+            if (tq * 128 + q >= g.len || n <= 0) continue;
+            uint8_t *p = d.values + (int64_t)(tq * 128 + q) * d.ld + line;
+            if (n >= 16) {
+                *reinterpret_cast<uint4 *>(p) = uint4{lo.x, lo.y, hi.x, hi.y};
+            } else {
+                store_bytes(p, lo, min(8, n));
+                store_bytes(p + 8, hi, min(8, n - 8));
+            }
         }
     }
 }
@@ -161,7 +192,6 @@ __global__ __launch_bounds__(256) void quantize_tile(QuantArgs g) {
 template <class T, int PER>
 __global__ __launch_bounds__(256) void quantize_rows(QuantArgs g) {
     const Dest &d = g.along;
-    const float top = d.format == O2M_FP8_E4M3 ? 448.0f : 57344.0f;
     const int lane16 = threadIdx.x & 15;
     const int64_t group = blockIdx.x * 16LL + (threadIdx.x >> 4);   // PER blocks of a line
     const int groups = (g.tiles_q + PER - 1) / PER;
@@ -169,29 +199,22 @@ __global__ __launch_bounds__(256) void quantize_rows(QuantArgs g) {
     if (p >= g.lines) return;
     const int blk0 = (int)(group % groups) * PER;
     const T *line = static_cast<const T *>(g.X) + p * g.ld;
-    float x[PER][8];
+    Run8<T> x[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int q0 = (blk0 + i) * 128 + 8 * lane16;
-        load8<T>(line + q0, min(8, g.len - q0), x[i]);
+        x[i] = load_run(line + q0, min(8, g.len - q0));
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        float m = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, magnitude(x[i][j]));
-#pragma unroll
-        for (int s = 1; s < 16; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
-        const Scale s = scale_of(m, d.format, d.scale_type);
+        uint32_t m = largest_of_16(largest_of(x[i]));
+        const bool fine = bits_finite<T>(m);
+        if (!fine) m = largest_of_16(largest_finite_of(x[i]));   // (the 16 lanes agree)
+        const Scale s = scale_of(bits_value<T>(m), d.format, d.scale_type);
         const int q0 = (blk0 + i) * 128 + 8 * lane16, n = g.len - q0;
         if (n <= 0) continue;
-        float y[4], z[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            y[j] = scaled(x[i][j], s.inv, top);
-            z[j] = scaled(x[i][4 + j], s.inv, top);
-        }
-        store_bytes(d.values + p * d.ld + q0, uint2{pack_fp8(y, d.format), pack_fp8(z, d.format)}, n);
+        const uint2 w = fine ? round_run<true>(x[i], s.inv, d.format) : round_run<false>(x[i], s.inv, d.format);
+        store_bytes(d.values + p * d.ld + q0, w, n);
         if (lane16 == 0) store_scale(d, p, blk0 + i, s.held);
     }
 }
@@ -206,7 +229,9 @@ Dest dest_of(const o2m_fp8_operand *o) {
 template <class T>
 hipError_t launch(const QuantArgs &g, int64_t tiles, hipStream_t st) {
     if (g.across.values || g.along.block != 1) {
-        quantize_tile<T><<<(unsigned)tiles, 256, 0, st>>>(g);
+        if (!g.across.values) quantize_tile<T, true, false><<<(unsigned)tiles, kTileThreads, 0, st>>>(g);
+        else if (!g.along.values) quantize_tile<T, false, true><<<(unsigned)tiles, kTileThreads, 0, st>>>(g);
+        else quantize_tile<T, true, true><<<(unsigned)tiles, kTileThreads, 0, st>>>(g);
         return hipGetLastError();
     }
     const int64_t by4 = ceil_div(g.lines * ceil_div(g.tiles_q, 4), 16), by1 = ceil_div((int64_t)g.lines * g.tiles_q, 16);
