@@ -56,6 +56,7 @@ _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _FORMATS = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
 _SCALES = {"pow2": 0, "float32": 1}
 _SCALE_DTYPES = {"pow2": torch.float8_e8m0fnu, "float32": torch.float32}
+_SCALE_KINDS = {torch.float8_e8m0fnu: 0, torch.uint8: 0, torch.float32: 1}
 BLOCK = 128
 
 
@@ -70,7 +71,7 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 
 
 def _here(x: torch.Tensor, name: str) -> None:
-    if not x.is_cuda or x.get_device() != _current_device():
+    if not x.is_cuda or x.get_device() != _current_device():   # (get_device() is -1 on the CPU)
         raise ValueError(f"{name} must be a tensor on the current device")
 
 
@@ -97,10 +98,14 @@ def _order(rows: int, cols: int, s0: int, s1: int, name: str):
 
 
 def _matrix(x: torch.Tensor, name: str):
-    if x.dim() != 2:
-        raise ValueError(f"{name} must be a matrix, got {x.dim()} dimensions")
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} must be a matrix, got {len(shape)} dimensions")
     _here(x, name)
-    return _order(x.size(0), x.size(1), x.stride(0), x.stride(1), name)
+    s0, s1 = x.stride()
+    if s1 == 1 and shape[0] > 1 and shape[1] > 1:
+        return b"R", s0
+    return _order(shape[0], shape[1], s0, s1, name)
 
 
 def _operand(x, name: str) -> _Operand:
@@ -109,32 +114,31 @@ def _operand(x, name: str) -> _Operand:
     fmt = _FORMATS.get(q.dtype)
     if fmt is None:
         raise TypeError(f"{name}: values must be float8_e4m3fn or float8_e5m2, got {q.dtype}")
-    if q.dim() != 2 or s.dim() != 2:
+    shape, s_shape = q.shape, s.shape
+    if len(shape) != 2 or len(s_shape) != 2:
         raise ValueError(f"{name}: values and scales must be matrices")
     _here(q, name)
     _here(s, name)
-    if s.dtype == torch.float32:
-        kind = 1
-    elif s.dtype == torch.float8_e8m0fnu or s.dtype == torch.uint8:
-        kind = 0
-    else:
+    kind = _SCALE_KINDS.get(s.dtype)
+    if kind is None:
         raise TypeError(f"{name}: scales must be float8_e8m0fnu (or its bytes) or float32, got {s.dtype}")
-    rows, k = q.shape
-    if k > 1 and rows > 0 and q.stride(1) != 1:
+    rows, k = shape
+    ld, step = q.stride()
+    if k > 1 and rows > 0 and step != 1:
         raise ValueError(f"{name}: the k values of a row must be contiguous (stride(1) == 1)")
-    ld = q.stride(0) if rows > 1 and k > 0 else (k + 15) // 16 * 16
-    if ld % 16 or q.data_ptr() % 16 or ld < k:
+    if rows <= 1 or k == 0:
+        ld = (k + 15) // 16 * 16
+    at = q.data_ptr()
+    if ld % 16 or at % 16 or ld < k:
         raise ValueError(f"{name}: rows must start at multiples of 16 bytes, one after another")
-    if s.size(1) != (k + BLOCK - 1) // BLOCK:
-        raise ValueError(f"{name}: {k} values a row need {(k + BLOCK - 1) // BLOCK} columns of scales, got {s.size(1)}")
-    if s.size(0) == rows:
-        block = 1
-    elif s.size(0) == (rows + BLOCK - 1) // BLOCK:
-        block = BLOCK
-    else:
-        raise ValueError(f"{name}: {rows} rows need {rows} or {(rows + BLOCK - 1) // BLOCK} rows of scales, "
-                         f"got {s.size(0)}")
-    return _Operand(q.data_ptr(), ld, s.data_ptr(), s.stride(0), s.stride(1), block, fmt, kind)
+    kb, rb = (k + BLOCK - 1) // BLOCK, (rows + BLOCK - 1) // BLOCK
+    r, columns = s_shape
+    if columns != kb:
+        raise ValueError(f"{name}: {k} values a row need {kb} columns of scales, got {columns}")
+    if r != rows and r != rb:
+        raise ValueError(f"{name}: {rows} rows need {rows} or {rb} rows of scales, got {r}")
+    s_row, s_blk = s.stride()
+    return _Operand(at, ld, s.data_ptr(), s_row, s_blk, 1 if r == rows else BLOCK, fmt, kind)
 
 
 def _empty(size, dtype, device, stream):
@@ -145,12 +149,12 @@ def _empty(size, dtype, device, stream):
         return torch.empty(size, dtype=dtype, device=device)
 
 
-def _scratch(nbytes: int, device, stream):
-    """(tensor that holds it, address, bytes) of scratch memory; torch's blocks
-    are 512-byte aligned."""
+def _scratch(nbytes: int, beside: torch.Tensor, stream):
+    """(tensor that holds it, address, bytes) of scratch memory on the device of
+    ``beside``; torch's blocks are 512-byte aligned."""
     if nbytes == 0:
         return None, None, 0
-    t = _empty((nbytes,), torch.uint8, device, stream)
+    t = _empty((nbytes,), torch.uint8, beside.device, stream)
     return t, t.data_ptr(), nbytes
 
 
@@ -248,11 +252,13 @@ def gemm_fp8(A, B, dtype=torch.bfloat16, out: torch.Tensor | None = None, accumu
         if dtype not in _TYPES:
             raise TypeError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
         out = _empty((m, n), dtype, A[0].device, stream)
-    elif tuple(out.shape) != (m, n):
-        raise ValueError(f"out must be of shape {(m, n)}, got {tuple(out.shape)}")
-    t = _type_of(out, "out")
-    order, ld = _matrix(out, "out")
-    ws, at, nbytes = _scratch(_L.o2m_gemm_fp8_workspace(m, n, k), out.device, stream)
+        t, order, ld = _TYPES[dtype], b"R", max(n, 1)
+    else:
+        if tuple(out.shape) != (m, n):
+            raise ValueError(f"out must be of shape {(m, n)}, got {tuple(out.shape)}")
+        t = _type_of(out, "out")
+        order, ld = _matrix(out, "out")
+    ws, at, nbytes = _scratch(_L.o2m_gemm_fp8_workspace(m, n, k), out, stream)
     _check(_L.o2m_gemm_fp8(m, n, k, a, b, out.data_ptr(), t, order, ld, int(accumulate), at,
                            nbytes, _stream(stream)), "gemm_fp8")
     return out
@@ -273,12 +279,14 @@ def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None)
         raise ValueError("X must be row-major")
     if out is None:
         out = _empty((tokens, n), X.dtype, X.device, stream)
-    elif tuple(out.shape) != (tokens, n) or out.dtype != X.dtype:
-        raise ValueError(f"out must be {X.dtype} of shape {(tokens, n)}")
-    order, ldy = _matrix(out, "out")
-    if order != b"R":
-        raise ValueError("out must be row-major")
-    ws, at, nbytes = _scratch(_L.o2m_linear_fp8_workspace(tokens, n, k), out.device, stream)
+        ldy = max(n, 1)
+    else:
+        if tuple(out.shape) != (tokens, n) or out.dtype != X.dtype:
+            raise ValueError(f"out must be {X.dtype} of shape {(tokens, n)}")
+        order, ldy = _matrix(out, "out")
+        if order != b"R":
+            raise ValueError("out must be row-major")
+    ws, at, nbytes = _scratch(_L.o2m_linear_fp8_workspace(tokens, n, k), out, stream)
     _check(_L.o2m_linear_fp8(tokens, n, k, X.data_ptr(), t, ldx, w, out.data_ptr(), ldy, at, nbytes,
                              _stream(stream)), "linear_fp8")
     return out
@@ -326,7 +334,7 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750
     if steps >= 0 and len(flat) != 3 * steps:
         raise ValueError(f"coefficients must be one triple or {steps} of them")
     coef = (ctypes.c_double * max(len(flat), 1))(*flat)
-    ws, at, nbytes = _scratch(_L.o2m_orthogonalize_workspace(batch, rows, cols, t), out.device, stream)
+    ws, at, nbytes = _scratch(_L.o2m_orthogonalize_workspace(batch, rows, cols, t), out, stream)
     _check(_L.o2m_orthogonalize(batch, rows, cols, G.data_ptr(), og, ldg, G.stride(0) if G.dim() == 3 else 0,
                                 out.data_ptr(), oo, ldo, out.stride(0) if G.dim() == 3 else 0, t, steps,
                                 ctypes.addressof(coef), eps, at, nbytes, _stream(stream)), "orthogonalize")
