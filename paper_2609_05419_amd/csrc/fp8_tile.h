@@ -108,7 +108,7 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
 #pragma unroll
         for (int c = 0; c < T::kCopyA; ++c) {
             const int q = wave * T::kCopyA + c;
-            copy_rows<0>(ra, buf + q * 1024, lane, q, (int)g.a.ld, kb * kStageRowBytes, left);
+            copy_rows<1>(ra, buf + q * 1024, lane, q, (int)g.a.ld, kb * kStageRowBytes, left);
         }
 #pragma unroll
         for (int c = 0; c < T::kCopyB; ++c) {
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
         else wait_vmem<0>();
         lds_barrier();
         if (left < kBlockK && (left & 15)) {   // uniform: the last stage of an odd k
-            if (tid < T::kRows) clear_row_tail(buf, tid, left, mine_a ? 0 : 2);
+            if (tid < T::kRows) clear_row_tail(buf, tid, left, mine_a ? 1 : 2);
             lds_barrier();
         }
         if (kb + S - 1 < s1) {
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
         }
 #pragma unroll
         for (int i = 0; i < M; ++i) {
-            const v8i fa = read_fragment<0>(buf, wi + 16 * i + q, lane);
+            const v8i fa = read_fragment<1>(buf, wi + 16 * i + q, lane);
             if constexpr (SUM == kScaled) {
                 const int ca = (int)sc[wi + 16 * i + q];
 #pragma unroll
@@ -241,10 +241,10 @@ hipError_t launch_tile(Fp8Args &g, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Tile sizes: 256 x 256 by 8 waves (kPartial; kScaled has a kernel of its own), 128 x
-// 128 by 4 (two workgroups per CU), 64 x 64 by 4 (two, with twice the stages on
+// Tile sizes: 256 x 256 by 8 waves (kPartial; kScaled has kernels of its own for this
+// and 256 x 128), 128 x 128 by 4 (two workgroups per CU), 64 x 64 by 4 (two, with twice the stages on
 // their way).
-enum TileSize { k256, k128, k64 };
+enum TileSize { k256, k256x128, k128, k64 };
 template <Sum SUM, int FA, int FB, bool WB>
 hipError_t launch_sizes(Fp8Args &g, TileSize size, hipStream_t st) {
     switch (size) {

@@ -27,6 +27,7 @@
 #include "fp8_tile.h"
 
 #include <algorithm>
+#include <stdlib.h>
 
 namespace o2m {
 namespace {
@@ -76,6 +77,7 @@ Plan plan_fp8(int m, int n, int k, bool wide) {
     p.per = kblocks;
     p.few = std::min(m, n) <= kFewRows;
     auto tiles = [&](int q) { return ceil_div(m, q) * ceil_div(n, q); };
+    if (const char *e = wide ? nullptr : getenv("O2M_T")) { p.size = (TileSize)atoi(e); return p; }
     p.size = tiles(256) >= 200 && !wide ? k256 : tiles(128) >= kCus ? k128 : k64;
     if (p.few || p.size != k64) return p;
     const int64_t want = std::min<int64_t>(kCus / std::min<int64_t>(tiles(64), kCus), std::max(1, kblocks / 4));
@@ -124,7 +126,7 @@ hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const 
     const int format = A.format * 2 + B.format;
     // the large kernel of power-of-two scales reads those of 8 rows at once
     auto fits = [](const Side &s) { return !s.by_row || (s.s_row == 1 && s.rows >= 8); };
-    const TileSize size = p.size == k256 && g.a.pow2 && !(fits(g.a) && fits(g.b)) ? k128 : p.size;
+    const TileSize size = p.size <= k256x128 && g.a.pow2 && !(fits(g.a) && fits(g.b)) ? k128 : p.size;
     const hipError_t e = type == O2M_TYPE_F32 ? launch_fp8_wide(g, format, size, st)
                          : g.a.pow2           ? launch_fp8_scaled(g, format, size, st)
                                               : launch_fp8_partial(g, format, size, st);

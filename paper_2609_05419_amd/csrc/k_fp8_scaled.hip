@@ -19,9 +19,9 @@ __device__ inline void mfma_scaled(v4f &d, const v8i &a, const v8i &b, int sa, i
                  : "memory");
 }
 
-// The scales of one operand for a wave: bytes of its lane's 8 rows, two dwords;
-// or, WHOLE, the one byte of its 128 rows.
-template <bool WHOLE>
+// The scales of one operand for a wave: bytes of its lane's N (8 or 4) rows, in
+// dwords; or, WHOLE, the one byte of its rows.
+template <bool WHOLE, int N>
 struct ScaleLane {
     typedef uint32_t v2u __attribute__((ext_vector_type(2)));
     const uint8_t *p;    // this lane's first byte in block 0
@@ -32,19 +32,22 @@ struct ScaleLane {
     int use[2];
     __device__ inline void init(const Side &s, int row) {
         s_blk = s.s_blk;
-        // the last lanes read the last 8 rows' scales and shift them into place
-        const int from = min(row, s.rows - 8);
-        shift = 8 * min(row - from, 7);
+        // the last lanes read the last N rows' scales and shift them into place
+        const int from = min(row, s.rows - N);
+        shift = 8 * min(row - from, N - 1);
         p = static_cast<const uint8_t *>(s.scales) + (WHOLE ? (int64_t)(min(row, s.rows - 1) >> 7) * s.s_row : from);
     }
     __device__ inline void fetch(int kb) {
         const uint8_t *at = p + kb * s_blk;
         if (WHOLE) next_one = *at;
-        else __builtin_memcpy(&next, at, 8);
+        else if (N == 8) __builtin_memcpy(&next, at, 8);
+        else __builtin_memcpy(&next_one, at, 4);
     }
     __device__ inline void begin() {
         if (WHOLE) {
             use[0] = use[1] = (int)(next_one * 0x01010101u);
+        } else if (N == 4) {
+            use[0] = (int)(next_one >> shift);
         } else {
             const uint64_t v = __builtin_bit_cast(uint64_t, next) >> shift;
             use[0] = (int)v;
@@ -53,10 +56,10 @@ struct ScaleLane {
     }
 };
 
-template <int FA, int FB, bool WA, bool WB>
+template <int FA, int FB, bool WA, bool WB, int N>
 struct ScaledOp {
-    ScaleLane<WA> a;
-    ScaleLane<WB> b;
+    ScaleLane<WA, 8> a;
+    ScaleLane<WB, N> b;
     int kblocks, k, lane;
     // (past the last stage: the last one's again, without a branch)
     __device__ inline void fetch(int s) {
@@ -67,7 +70,8 @@ struct ScaledOp {
         a.begin();
         b.begin();
         // VALU results before an MFMA of the assembly below reads them
-        asm volatile("s_nop 1" : "+v"(a.use[0]), "+v"(a.use[1]), "+v"(b.use[0]), "+v"(b.use[1]));
+        asm volatile("s_nop 1" : "+v"(a.use[0]), "+v"(a.use[1]), "+v"(b.use[0]));
+        if constexpr (N == 8) asm volatile("s_nop 1" : "+v"(b.use[1]));
     }
     static constexpr int kParts = 1;
     template <int I, int J, int P>
@@ -98,42 +102,48 @@ struct Fp8Src {
     __device__ inline int left(int s) const { return kbytes - s * kBlockK; }
 };
 
-template <int FA, int FB, bool WA, bool WB>
+template <int FA, int FB, bool WA, bool WB, int N>
 __global__ __launch_bounds__(256, 1) void fp8_pipe(Fp8Args g) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kPipeLds];
-    const PipeWave w = pipe_wave(lds);
+    typedef PipeShape<N> T;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+    const PipeWave w = pipe_wave<N>(lds);
     const TileCoord tc = tile_of(blockIdx.x & 7, blockIdx.x >> 3, g.mt, g.nt, g.chunk, 0);
     if (!tc.valid) return;   // whole workgroup
-    const int i0 = tc.ti * kPipeTile, j0 = tc.tj * kPipeTile;
+    const int i0 = tc.ti * kPipeTile, j0 = tc.tj * T::kTn;
     const Fp8Src src = {rows_of(g.a.values + i0 * g.a.ld, min(kPipeTile, g.a.rows - i0), g.a.ld, g.k),
-                        rows_of(g.b.values + j0 * g.b.ld, min(kPipeTile, g.b.rows - j0), g.b.ld, g.k), (int)g.a.ld,
+                        rows_of(g.b.values + j0 * g.b.ld, min(T::kTn, g.b.rows - j0), g.b.ld, g.k), (int)g.a.ld,
                         (int)g.b.ld, g.k};
-    ScaledOp<FA, FB, WA, WB> op;
+    ScaledOp<FA, FB, WA, WB, N> op;
     op.kblocks = g.kblocks;
     op.k = g.k;
     op.lane = w.lane;
     const int q = w.lane & 15;
     op.a.init(g.a, i0 + w.row_a + 8 * q);
-    op.b.init(g.b, j0 + w.row_b + 8 * q);
-    v4f acc[8][8];
-    pipe_run(w, op, src, g.kblocks, acc);
-    pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) { store_run<8>(g, i0 + row, j0 + col, v); });
+    op.b.init(g.b, j0 + w.row_b + N * q);
+    v4f acc[8][N];
+    pipe_run<N>(w, op, src, g.kblocks, acc);
+    pipe_results<false, N>(w, acc, [&](int row, int col, const auto &v) { store_run<N>(g, i0 + row, j0 + col, v); });
 }
 
-template <int FA, int FB>
-hipError_t launch(Fp8Args &g, TileSize size, hipStream_t st) {
-    if (size != k256) return launch_sizes<kScaled, FA, FB, false>(g, size, st);
+template <int FA, int FB, int N>
+hipError_t launch_pipe(Fp8Args &g, hipStream_t st) {
     g.mt = (int)ceil_div(g.a.rows, kPipeTile);
-    g.nt = (int)ceil_div(g.b.rows, kPipeTile);
+    g.nt = (int)ceil_div(g.b.rows, PipeShape<N>::kTn);
     const int64_t chunk = ceil_div((int64_t)g.mt * g.nt, kXcds);
     if (kXcds * chunk > 0x7FFFFFFF) return hipErrorInvalidValue;
     g.chunk = (int)chunk;
     const unsigned grid = (unsigned)(kXcds * chunk);
-    if (g.a.by_row && g.b.by_row) fp8_pipe<FA, FB, false, false><<<grid, 256, 0, st>>>(g);
-    else if (g.a.by_row) fp8_pipe<FA, FB, false, true><<<grid, 256, 0, st>>>(g);
-    else if (g.b.by_row) fp8_pipe<FA, FB, true, false><<<grid, 256, 0, st>>>(g);
-    else fp8_pipe<FA, FB, true, true><<<grid, 256, 0, st>>>(g);
+    if (g.a.by_row && g.b.by_row) fp8_pipe<FA, FB, false, false, N><<<grid, 256, 0, st>>>(g);
+    else if (g.a.by_row) fp8_pipe<FA, FB, false, true, N><<<grid, 256, 0, st>>>(g);
+    else if (g.b.by_row) fp8_pipe<FA, FB, true, false, N><<<grid, 256, 0, st>>>(g);
+    else fp8_pipe<FA, FB, true, true, N><<<grid, 256, 0, st>>>(g);
     return hipGetLastError();
+}
+
+template <int FA, int FB>
+hipError_t launch(Fp8Args &g, TileSize size, hipStream_t st) {
+    return size == k256 ? launch_pipe<FA, FB, 8>(g, st) : size == k256x128 ? launch_pipe<FA, FB, 4>(g, st)
+                                                                          : launch_sizes<kScaled, FA, FB, false>(g, size, st);
 }
 
 }  // namespace

@@ -303,8 +303,9 @@ __device__ inline float *part_of(const ProductArgs &g, int z, int b) {
 
 template <bool SPLIT, Product KIND>
 __global__ __launch_bounds__(256, 1) void product_pipe(ProductArgs g) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kPipeLds];
-    const PipeWave w = pipe_wave(lds);
+    // (squares for the symmetric products)
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[PipeShape<8>::kLds];
+    const PipeWave w = pipe_wave<8>(lds);
     const int64_t slot = (int64_t)(blockIdx.x & 7) * g.chunk + (blockIdx.x >> 3);
     const int z = (int)(slot % g.splits);
     int b, ti, tj;
@@ -313,19 +314,19 @@ __global__ __launch_bounds__(256, 1) void product_pipe(ProductArgs g) {
     const HalfSrc<SPLIT> src(g, b, i0, j0, kPipeTile, kPipeTile, z);
     HalfOp op;
     v4f acc[8][8];
-    pipe_run(w, op, src, src.total, acc);
+    pipe_run<8>(w, op, src, src.total, acc);
     if (g.splits > 1) {
         float *part = part_of(g, z, b);
-        pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) {
+        pipe_results<false, 8>(w, acc, [&](int row, int col, const v8f &v) {
             if (i0 + row < g.rows && j0 + col < g.cols)
                 *reinterpret_cast<v8f *>(part + (int64_t)(i0 + row) * g.cols + j0 + col) = v;
         });
         return;
     }
     if (writes_rows<KIND>(g))
-        pipe_results<false>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, false, 8>(g, b, i0 + row, j0 + col, v); });
+        pipe_results<false, 8>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, false, 8>(g, b, i0 + row, j0 + col, v); });
     if (writes_across<KIND>(g, ti, tj))
-        pipe_results<true>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, true, 8>(g, b, i0 + row, j0 + col, v); });
+        pipe_results<true, 8>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, true, 8>(g, b, i0 + row, j0 + col, v); });
 }
 
 // Smaller tiles: WR x WC waves of M x 4 blocks, a ring of S stage buffers with S - 1
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product_tile(ProductArgs g) {
 #pragma unroll
         for (int c = 0; c < kCopyA; ++c) {
             const int q = wave * kCopyA + c;
-            copy_rows<0>(src.rp, buf + q * 1024, lane, q, src.ld_a, at_a, kStageRowBytes);
+            copy_rows<1>(src.rp, buf + q * 1024, lane, q, src.ld_a, at_a, kStageRowBytes);
         }
 #pragma unroll
         for (int c = 0; c < kCopyB; ++c) {
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product_tile(ProductArgs g) {
         for (int j = 0; j < 4; ++j) fb[j] = read_fragment<2>(buf + kTm * kStageRowBytes, wj + 4 * q + j, lane);
 #pragma unroll
         for (int i = 0; i < M; ++i) {
-            const v8i fa = read_fragment<0>(buf, wi + 16 * i + q, lane);
+            const v8i fa = read_fragment<1>(buf, wi + 16 * i + q, lane);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
