@@ -22,12 +22,11 @@
 //   fp32 results                       k_fp8_wide.hip
 //   power-of-two scales                k_fp8_scaled.hip
 //   fp32 scales                        k_fp8_partial.hip
-// Products with too few tiles of 128 x 128 to fill the part are split along k, and
-// join_parts adds the fp32 sums up in a fixed order.
+// Products with too few tiles to fill the part are split along k, and join_parts
+// adds the fp32 sums up in a fixed order.
 #include "fp8_tile.h"
 
 #include <algorithm>
-#include <stdlib.h>
 
 namespace o2m {
 namespace {
@@ -53,37 +52,75 @@ __global__ __launch_bounds__(256) void zero_out(T *C, int64_t m, int64_t total, 
 
 constexpr int kFewRows = 32;
 
-// The tiles of a launch, by how many there are.  Measured (us, power-of-two scales,
-// bf16; tiles of 256 x 256, 128 x 128, 64 x 64):
-//   4096 x 4096 x 4096   54    78   139      2048 x 2048 x 2048   28   19   23
-//   4096 x 4096 x 512    19    21    33      1000 x 1000 x 1000   21   11    7
-//   2048 x 4096 x 8192   79    77   132      512 x 2048 x 2048    27   17   10
-// (fp32 scales 4096^3 72, 86, 146.)  fp32 results take 128 x 128 for the largest too:
-// the widened fragments leave no registers for more (4096^3 145 us, with 256 x
-// 256 and registers spilled 151).  Tiles of 64 x 64 that leave CUs idle are split
-// along k until each has one, from 4 stages each: 300 x 300 x 8000 (25 tiles) 30 us
-// in one piece, 11.5 in 8; 64 x 4096 x 4096 (64) 16 and 10.7 in 4; 300 x 1283 x 2051
-// (105) 12.4 and 10.6 in 2; with 256 tiles the joining costs more than it brings
-// (1000^3 6.9 and 12.1).
+// Tiles and splits of a launch: those with the least estimated time (us), a round of
+// workgroups after the other.  A size has `fixed` per round (its first copies and
+// its results), and per stage `one` while a CU has one workgroup, `full` with all
+// of `resident` (of one resident: while few CUs work, and when all do, which
+// lowers the clock).  Fitted to 37 products of 13 shapes, of which the measured
+// best or one within 3% of it is taken but for 1537 x 1283 x 2051, whose rows of odd
+// lengths cost more (8%).  Measured (us; tiles of 256 x 256, 256 x 128, 128 x 128,
+// 64 x 64):
+//   power-of-two scales      4096 x 4096 x 4096     56    71    80   133
+//                            3000 x 3000 x 3000     42    56    52    65
+//                            2048 x 4096 x 8192     81    63    73   125
+//                            2048 x 2048 x 2048     29    21    19    22
+//                            1000 x 1000 x 1000     22    16    11     7
+//   fp32 scales              4096 x 4096 x 4096     75          86   143
+//                            2048 x 4096 x 8192    124          87   136
+//   fp32 results             4096 x 4096 x 4096                140   222
+//                            512 x 2048 x 2048                  25    15
+// (fp32 results: the widened fragments leave no registers for tiles of 256 x 256,
+// which took 151 us with spilled ones.)  Tiles of 64 x 64 that leave CUs idle are
+// split along k, from 4 stages each: 300 x 300 x 8000 (25 tiles) 30 us in one piece,
+// 11.5 in 8; 64 x 4096 x 4096 (64) 16, and 10.7 in 4; 1000 x 1000 x 1000 (256) 6.9, and
+// 12.1 in 2.
 struct Plan {
     bool few;
     TileSize size;
     int splits, per;
 };
-Plan plan_fp8(int m, int n, int k, bool wide) {
-    Plan p = {};
+struct TileCost {
+    TileSize size;
+    int rows, cols, resident;
+    double fixed, one, full;
+};
+constexpr TileCost kCosts[3][4] = {
+    {{k256, 256, 256, 1, 13.0, 1.00, 1.33}, {k256x128, 256, 128, 1, 9.5, 0.69, 0.82},
+     {k128, 128, 128, 2, 6.5, 0.70, 1.03}, {k64, 64, 64, 2, 3.5, 0.37, 0.45}},
+    {{k256, 256, 256, 1, 11.0, 1.70, 2.00}, {}, {k128, 128, 128, 2, 6.5, 0.84, 1.24}, {k64, 64, 64, 2, 3.7, 0.42, 0.51}},
+    {{}, {}, {k128, 128, 128, 2, 8.0, 1.22, 1.98}, {k64, 64, 64, 2, 4.2, 0.66, 0.82}}};
+
+Plan plan_fp8(int m, int n, int k, Sum sum) {
     const int kblocks = (int)ceil_div(k, kBlockK);
-    p.splits = 1;
-    p.per = kblocks;
-    p.few = std::min(m, n) <= kFewRows;
-    auto tiles = [&](int q) { return ceil_div(m, q) * ceil_div(n, q); };
-    if (const char *e = wide ? nullptr : getenv("O2M_T")) { p.size = (TileSize)atoi(e); return p; }
-    p.size = tiles(256) >= 200 && !wide ? k256 : tiles(128) >= kCus ? k128 : k64;
-    if (p.few || p.size != k64) return p;
-    const int64_t want = std::min<int64_t>(kCus / std::min<int64_t>(tiles(64), kCus), std::max(1, kblocks / 4));
-    p.per = (int)ceil_div(kblocks, want);
-    p.splits = (int)ceil_div(kblocks, p.per);
-    return p;
+    Plan best = {};
+    best.splits = 1;
+    best.per = kblocks;
+    best.few = std::min(m, n) <= kFewRows;
+    if (best.few) return best;
+    double least = 0.0;
+    for (const TileCost &s : kCosts[sum]) {
+        if (!s.rows) continue;
+        for (int want = 1; want <= 16; want *= 2) {
+            if (want > 1 && (s.size != k64 || kblocks < 4 * want)) break;
+            Plan p = {};
+            p.size = s.size;
+            p.per = (int)ceil_div(kblocks, want);
+            p.splits = (int)ceil_div(kblocks, p.per);
+            const int64_t groups = ceil_div(m, s.rows) * ceil_div(n, s.cols) * p.splits;
+            const int64_t round = (int64_t)kCus * s.resident, rest = groups % round;
+            double t = (double)(groups / round) * (s.fixed + p.per * s.full);
+            if (rest > 0) {
+                const double fill = s.resident == 1 ? (double)rest / kCus : rest > kCus ? 1.0 : 0.0;
+                t += s.fixed + p.per * (s.one + (s.full - s.one) * fill);
+            }
+            if (p.splits > 1) t += 3.0 + p.splits * (0.15 + 0.8e-6 * m * n);   // join_parts
+            if (least == 0.0 || t < least) {
+                least = t;
+                best = p;
+            }
+        }
+    }
+    return best;
 }
 
 }  // namespace
@@ -99,14 +136,16 @@ hipError_t launch_zero_out(void *C, int64_t m, int64_t n, int64_t ldc, int size,
 
 size_t gemm_fp8_workspace(int m, int n, int k) {
     // either order of the result: its rows are those of one operand or the other
-    const Plan p = plan_fp8(m, n, k, false);   // (the same splits for every type)
-    if (p.splits == 1) return 0;
-    return sizeof(float) * (size_t)p.splits * (size_t)std::max(m * round_up64(n, 4), n * round_up64(m, 4));
+    int splits = 1;
+    for (const Sum sum : {kScaled, kPartial, kWide})
+        splits = std::max({splits, plan_fp8(m, n, k, sum).splits, plan_fp8(n, m, k, sum).splits});
+    if (splits == 1) return 0;
+    return sizeof(float) * (size_t)splits * (size_t)std::max(m * round_up64(n, 4), n * round_up64(m, 4));
 }
 
 hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const o2m_fp8_operand &B, void *C, int type,
                            int64_t ldc, bool accumulate, void *ws, hipStream_t st) {
-    const Plan p = plan_fp8(m, n, k, type == O2M_TYPE_F32);
+    const Plan p = plan_fp8(m, n, k, type == O2M_TYPE_F32 ? kWide : A.scale_type == O2M_SCALES_POW2 ? kScaled : kPartial);
     if (p.few)
         return n <= m ? launch_few(n, m, k, B, A, C, type, 1, ldc, accumulate, st)
                       : launch_few(m, n, k, A, B, C, type, ldc, 1, accumulate, st);

@@ -139,7 +139,8 @@ def test_gemm(o2m, m, n, k, scales):
 
 @pytest.mark.parametrize("m,n,k", [(1290, 1601, 128), (1290, 1601, 97), (1537, 1283, 300), (1536, 2048, 256), (1400, 1900, 1041),
                                    (8, 8200, 700), (9000, 130, 2064), (2100, 2000, 200), (2065, 2100, 333),
-                                   (3700, 3601, 128), (3700, 3601, 97), (3601, 3700, 300), (3590, 3800, 1041), (140, 60001, 264)])
+                                   (3700, 3601, 128), (3700, 3601, 97), (3601, 3700, 300), (3590, 3800, 1041), (140, 60001, 264),
+                                   (2000, 4001, 2051), (1800, 4090, 1930), (4080, 2000, 2304)])
 @pytest.mark.parametrize("scales", ["pow2", "float32"])
 def test_gemm_large(o2m, m, n, k, scales):
     """Enough tiles for the kernels of larger products: one stage and many, odd and
