@@ -157,10 +157,15 @@ struct ProductArgs {
     int rows, cols;
     int kblocks;        // stages of 64
     int mt, nt, tiles;  // tiles of the launch's size; per matrix
-    int batch, chunk;   // chunk: tiles of the whole launch per XCD
+    int tm, tn;         // that size
+    int batch;
     float diag, add, mul;
-    float *parts;       // split launches: sums [split][batch][rows][cols]
-    int splits, per;    // stages of a split
+    // Workgroups: one for each of the first `whole` tiles, then `splits` for each of the
+    // `rest`, `per` stages each, whose sums go to parts [rest][splits][tm][tn].
+    int64_t whole, rest;
+    int whole_chunk, rest_chunk;   // workgroups of each kind per XCD
+    int splits, per;
+    float *parts;
     void *O;            // kLast: where the r x c result goes
     int64_t o_row, o_col, o_batch;
     int r, c, type;
@@ -175,20 +180,48 @@ __device__ inline void triangle_tile(int t, int &ti, int &tj) {
     tj = t - ti * (ti + 1) / 2;
 }
 
-// Matrix and tile of slot t of a launch; tiles of one matrix in groups of 8
+// Matrix and place of tile t of a launch; tiles of one matrix in groups of 8
 // tile-rows (tile_schedule.h), or a triangle.
 template <Product KIND>
-__device__ inline bool tile_at(const ProductArgs &g, int64_t t, int mt, int nt, int tiles, int &b, int &ti, int &tj) {
-    b = (int)(t / tiles);
-    if (b >= g.batch) return false;
-    const int in = (int)(t % tiles);
+__device__ inline void tile_at(const ProductArgs &g, int64_t t, int &b, int &ti, int &tj) {
+    b = (int)(t / g.tiles);
+    const int in = (int)(t % g.tiles);
     if (symmetric(KIND)) {
         triangle_tile(in, ti, tj);
-        return true;
+        return;
     }
-    const TileCoord c = tile_of(0, in, mt, nt, tiles, 0);
+    const TileCoord c = tile_of(0, in, g.mt, g.nt, g.tiles, 0);
     ti = c.ti;
     tj = c.tj;
+}
+
+// What a workgroup computes.  An XCD has neighbouring tiles, and of split ones those of
+// the same stages.
+struct Share {
+    int b, ti, tj;
+    int first, total;   // stages
+    float *part;        // where the sums go; null: the whole product
+};
+template <Product KIND>
+__device__ inline bool share_of(const ProductArgs &g, int stages, Share &w) {
+    const int xcd = blockIdx.x % kXcds, slot = blockIdx.x / kXcds;
+    int64_t t;
+    if (slot < g.whole_chunk) {
+        t = (int64_t)xcd * g.whole_chunk + slot;
+        if (t >= g.whole) return false;
+        w.first = 0;
+        w.total = stages;
+        w.part = nullptr;
+    } else {
+        t = (int64_t)xcd * g.rest_chunk + slot - g.whole_chunk;
+        if (t >= g.rest * g.splits) return false;
+        const int64_t z = t / g.rest, u = t % g.rest;
+        w.first = (int)z * g.per;
+        w.total = min(g.per, stages - w.first);
+        w.part = g.parts + (u * g.splits + z) * g.tm * g.tn;
+        t = g.whole + u;
+    }
+    tile_at<KIND>(g, t, w.b, w.ti, w.tj);
     return true;
 }
 
@@ -201,10 +234,11 @@ struct HalfSrc {
     // see, and not zeros)
     __amdgpu_buffer_rsrc_t rp, rq;
     int ld_a, ld_b, lo_a, lo_b, kblocks, first, total;
-    __device__ inline HalfSrc(const ProductArgs &g, int b, int i0, int j0, int tile_m, int tile_n, int z) {
+    __device__ inline HalfSrc(const ProductArgs &g, const Share &w, int i0, int j0, int tile_m, int tile_n) {
+        const int b = w.b;
         kblocks = g.kblocks;
-        first = z * g.per;
-        total = min(g.per, (SPLIT ? 3 : 1) * kblocks - first);
+        first = w.first;
+        total = w.total;
         ld_a = (int)g.p.pitch * 2;
         ld_b = (int)g.q.pitch * 2;
         lo_a = (int)g.p.lo * 2;
@@ -297,36 +331,29 @@ __device__ inline bool writes_across(const ProductArgs &g, int ti, int tj) {
     return symmetric(KIND) ? ti != tj : KIND != kLast || g.o_col != 1;
 }
 
-__device__ inline float *part_of(const ProductArgs &g, int z, int b) {
-    return g.parts + ((int64_t)z * g.batch + b) * g.rows * g.cols;
-}
-
-template <bool SPLIT, Product KIND>
+template <bool SPLIT, Product KIND, int N>
 __global__ __launch_bounds__(256, 1) void product_pipe(ProductArgs g) {
-    // (squares for the symmetric products)
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[PipeShape<8>::kLds];
-    const PipeWave w = pipe_wave<8>(lds);
-    const int64_t slot = (int64_t)(blockIdx.x & 7) * g.chunk + (blockIdx.x >> 3);
-    const int z = (int)(slot % g.splits);
-    int b, ti, tj;
-    if (!tile_at<KIND>(g, slot / g.splits, g.mt, g.nt, g.tiles, b, ti, tj)) return;
-    const int i0 = ti * kPipeTile, j0 = tj * kPipeTile;
-    const HalfSrc<SPLIT> src(g, b, i0, j0, kPipeTile, kPipeTile, z);
+    static_assert(N == 8 || !symmetric(KIND), "triangles of squares");
+    typedef PipeShape<N> T;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::kLds];
+    const PipeWave w = pipe_wave<N>(lds);
+    Share of;
+    if (!share_of<KIND>(g, (SPLIT ? 3 : 1) * g.kblocks, of)) return;   // whole workgroup
+    const int b = of.b, i0 = of.ti * kPipeTile, j0 = of.tj * T::kTn;
+    const HalfSrc<SPLIT> src(g, of, i0, j0, kPipeTile, T::kTn);
     HalfOp op;
-    v4f acc[8][8];
-    pipe_run<8>(w, op, src, src.total, acc);
-    if (g.splits > 1) {
-        float *part = part_of(g, z, b);
-        pipe_results<false, 8>(w, acc, [&](int row, int col, const v8f &v) {
-            if (i0 + row < g.rows && j0 + col < g.cols)
-                *reinterpret_cast<v8f *>(part + (int64_t)(i0 + row) * g.cols + j0 + col) = v;
+    v4f acc[8][N];
+    pipe_run<N>(w, op, src, src.total, acc);
+    if (of.part) {
+        pipe_results<false, N>(w, acc, [&](int row, int col, const auto &v) {
+            __builtin_memcpy(of.part + row * T::kTn + col, &v, sizeof v);
         });
         return;
     }
     if (writes_rows<KIND>(g))
-        pipe_results<false, 8>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, false, 8>(g, b, i0 + row, j0 + col, v); });
-    if (writes_across<KIND>(g, ti, tj))
-        pipe_results<true, 8>(w, acc, [&](int row, int col, const v8f &v) { emit<SPLIT, KIND, true, 8>(g, b, i0 + row, j0 + col, v); });
+        pipe_results<false, N>(w, acc, [&](int row, int col, const auto &v) { emit<SPLIT, KIND, false, N>(g, b, i0 + row, j0 + col, v); });
+    if (writes_across<KIND>(g, of.ti, of.tj))
+        pipe_results<true, N>(w, acc, [&](int row, int col, const auto &v) { emit<SPLIT, KIND, true, 8>(g, b, i0 + row, j0 + col, v); });
 }
 
 // Smaller tiles: WR x WC waves of M x 4 blocks, a ring of S stage buffers with S - 1
@@ -339,11 +366,10 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product_tile(ProductArgs g) {
     constexpr int kCopyA = kTm / 8 / kWaves, kCopyB = kTn / 8 / kWaves;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S * kBuf];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int z = blockIdx.x % g.splits;
-    int b, ti, tj;
-    if (!tile_at<KIND>(g, blockIdx.x / g.splits, g.mt, g.nt, g.tiles, b, ti, tj)) return;
-    const int i0 = ti * kTm, j0 = tj * kTn;
-    const HalfSrc<SPLIT> src(g, b, i0, j0, kTm, kTn, z);
+    Share of;
+    if (!share_of<KIND>(g, (SPLIT ? 3 : 1) * g.kblocks, of)) return;   // whole workgroup
+    const int b = of.b, i0 = of.ti * kTm, j0 = of.tj * kTn;
+    const HalfSrc<SPLIT> src(g, of, i0, j0, kTm, kTn);
     auto copy = [&](int s, uint8_t *buf) {
         const int at_a = src.at_a(s), at_b = src.at_b(s);
 #pragma unroll
@@ -391,9 +417,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product_tile(ProductArgs g) {
         }
         u = u + 1 == S ? 0 : u + 1;
     }
-    const bool whole = g.splits == 1;
-    const bool rows = !whole || writes_rows<KIND>(g), across = whole && writes_across<KIND>(g, ti, tj);
-    float *part = part_of(g, z, b);
+    const bool rows = of.part || writes_rows<KIND>(g), across = !of.part && writes_across<KIND>(g, of.ti, of.tj);
 #pragma unroll
     for (int i = 0; i < M; ++i) {
         const int row = i0 + wi + 16 * i + 4 * (lane >> 4), col = j0 + wj + 4 * q;
@@ -401,9 +425,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product_tile(ProductArgs g) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const v4f v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
-                if (whole) emit<SPLIT, KIND, false, 4>(g, b, row + e, col, v);
-                else if (row + e < g.rows && col < g.cols)
-                    *reinterpret_cast<v4f *>(part + (int64_t)(row + e) * g.cols + col) = v;
+                if (of.part) *reinterpret_cast<v4f *>(of.part + (row + e - i0) * kTn + col - j0) = v;
+                else emit<SPLIT, KIND, false, 4>(g, b, row + e, col, v);
             }
         if (across)
 #pragma unroll
@@ -411,42 +434,38 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product_tile(ProductArgs g) {
     }
 }
 
-// Adds up the splits in their order and writes D and its transpose, 64 x 64 per
-// workgroup.
+// Adds up the splits in their order and writes D and its transpose, 32 x 64 of a tile
+// per workgroup.
 template <bool SPLIT, Product KIND>
 __global__ __launch_bounds__(256) void product_join(ProductArgs g) {
-    __shared__ float tile[64][65];
-    const int tid = threadIdx.x, mt = g.rows / 64, nt = g.cols / 64;
+    __shared__ float tile[32][65];
+    const int tid = threadIdx.x, across_tile = g.tn / 64, per_tile = g.tm / 32 * across_tile;
+    const int64_t u = blockIdx.x / per_tile;
+    const int in = blockIdx.x % per_tile, di = in / across_tile * 32, dj = in % across_tile * 64;
     int b, ti, tj;
-    if (!tile_at<KIND>(g, blockIdx.x, mt, nt, symmetric(KIND) ? mt * (mt + 1) / 2 : mt * nt, b, ti, tj)) return;
-    const int i0 = ti * 64, j0 = tj * 64;
+    tile_at<KIND>(g, g.whole + u, b, ti, tj);
+    const int i0 = ti * g.tm + di, j0 = tj * g.tn + dj;
+    if (i0 >= g.rows || j0 >= g.cols) return;   // whole workgroup
     const bool rows = writes_rows<KIND>(g), across = writes_across<KIND>(g, ti, tj);
-    const int64_t plane = (int64_t)g.batch * g.rows * g.cols;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int row = 32 * h + (tid >> 3), col = (tid & 7) * 8;
-        const float *at = part_of(g, 0, b) + (int64_t)(i0 + row) * g.cols + j0 + col;
-        v4f lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-        for (int z = 0; z < g.splits; ++z) {
-            lo += *reinterpret_cast<const v4f *>(at + z * plane);
-            hi += *reinterpret_cast<const v4f *>(at + z * plane + 4);
-        }
-        const v8f v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        if (rows) emit<SPLIT, KIND, false, 8>(g, b, i0 + row, j0 + col, v);
-        if (across)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) tile[row][col + j] = v[j];
+    const int row = tid >> 3, col = (tid & 7) * 8, plane = g.tm * g.tn;
+    const float *at = g.parts + u * g.splits * plane + (di + row) * g.tn + dj + col;
+    v4f lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int z = 0; z < g.splits; ++z) {
+        lo += *reinterpret_cast<const v4f *>(at + (int64_t)z * plane);
+        hi += *reinterpret_cast<const v4f *>(at + (int64_t)z * plane + 4);
     }
+    const v8f v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    if (rows) emit<SPLIT, KIND, false, 8>(g, b, i0 + row, j0 + col, v);
     if (!across) return;   // uniform over the workgroup
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tile[row][col + j] = v[j];
     __syncthreads();
+    const int down = (tid & 3) * 8;
+    v8f t;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int col = 32 * h + (tid >> 3), row = (tid & 7) * 8;
-        v8f v;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = tile[row + i][col];
-        emit<SPLIT, KIND, true, 8>(g, b, i0 + row, j0 + col, v);
-    }
+    for (int i = 0; i < 8; ++i) t[i] = tile[down + i][tid >> 2];
+    emit<SPLIT, KIND, true, 8>(g, b, i0 + down, j0 + (tid >> 2), t);
 }
 
 // No steps: X itself.
@@ -470,47 +489,64 @@ struct Buffers {
 
 // How a product of rows x cols (padded) and `stages` stages is launched.
 struct ProductPlan {
-    int size;            // tile rows and columns: 256 (the pipeline), 128 or 64
-    int mt, nt, tiles;   // per matrix
+    int tm, tn;                   // tiles: 256 x 256, 256 x 128 (the pipeline), 128 x 128, 64 x 64
+    int mt, nt, tiles;            // per matrix
+    int64_t whole, rest;          // tiles with one workgroup, and split ones
     int splits, per;
 };
-// The time of a launch is estimated (us) from its workgroups W and the stages n of
-// each: W / 512 rounds of two workgroups per CU (the pipeline: W / 256 of one),
-// `pair` a stage with both in place and `one` with one, then the writing, or, of a
-// split launch, the sums' way through memory and the joining.  Measured, and the
-// estimate's choice within 10% of the best of 18 launches each:
-//   r = c = 2048, one part, A: 64 28 us, 128 25, 128 in 2 splits 24, 256 50
-//   r = c = 4096, one part, A: 128 102, 256 96;  two parts: 128 321, in 2 splits 265
-//   r = c = 1024, two parts, A: 64 21, 128 in 4 splits 20, 256 96
-//   300 x 900, two parts, A: 64 20, in 4 splits 12, 128 in 4 splits 17
+// The tiles, and how many of them are split along k: all, or those of the last round
+// that leaves CUs idle, or none, whichever has the least estimated time (us).  A size
+// has `fixed`, then per stage `one` while a CU has one workgroup and `full` with all of
+// `resident` (of one resident: while few CUs work, and when all do); then the
+// writing, or the sums' way through memory and their joining.  Fitted to the best of
+// 10 to 60 launches each of 54 products (64 x 64 tiles a, 128 x 128 b, 256 x 128 c, 256 x
+// 256 d; /n: split in n, +/n: the last round's); what it takes is 0.4% slower than the
+// best on average, 8% at most.  Measured (us):
+//   r = c = 4096, one part, A    d 93, b 100, b/2 102, b+/8 77, b+/2 87
+//                           X    d 108, b 123, c 126
+//   r = c = 2048, one part, A    b 25, a 27, b/2 24, a+/8 24;  two parts: b/3 45, c/6 54
+//   1024 x 8192, two parts, A    b/12 47, b/8 56, d/12 65;  X: c 62, b 64, d 93
+//   r = c = 1024, two parts, A   a/3 18, b/4 18, a 29
+//   320 x 896, two parts, A      a/4 11, a 22, b/4 16
 ProductPlan plan_product(int batch, int rows, int cols, int stages, bool sym) {
     struct Size {
-        int size, resident;
-        double fixed, one, pair;
+        int tm, tn, resident;
+        double fixed, one, full;
     };
-    constexpr Size sizes[] = {{64, 2, 2.5, 0.42, 0.60}, {128, 2, 3.0, 0.68, 1.06}, {kPipeTile, 1, 6.0, 1.40, 1.40}};
+    constexpr Size sizes[] = {{64, 64, 2, 2.5, 0.42, 0.44}, {128, 128, 2, 3.9, 0.74, 0.90}, {256, 128, 1, 4.6, 0.89, 0.89},
+                              {256, 256, 1, 8.1, 1.21, 1.65}};
     const double entries = (double)batch * rows * cols * (sym ? 0.5 : 1.0);
     ProductPlan best = {};
     double least = 0.0;
-    for (const Size &s : sizes)
-        for (int want = 1; want <= 16; want *= 2) {
-            ProductPlan p;
-            p.size = s.size;
-            p.mt = (int)ceil_div(rows, s.size);
-            p.nt = (int)ceil_div(cols, s.size);
-            p.tiles = sym ? p.mt * (p.mt + 1) / 2 : p.mt * p.nt;
-            p.per = (int)ceil_div(stages, want);
-            p.splits = (int)ceil_div(stages, p.per);
-            if (want > 1 && p.per < 4) break;
-            const int64_t groups = (int64_t)p.tiles * batch * p.splits, round = (int64_t)kCus * s.resident, rest = groups % round;
-            double t = s.fixed + p.per * (groups / round * s.pair + (rest > kCus ? s.pair : rest > 0 ? s.one : 0.0));
-            t += entries * 2e-6;
-            if (p.splits > 1) t += 3.0 + 0.6 * p.splits + p.splits * entries * 0.8e-6;
-            if (best.tiles == 0 || t < least) {
-                least = t;
-                best = p;
+    for (const Size &s : sizes) {
+        if (sym && s.tm != s.tn) continue;
+        ProductPlan p;
+        p.tm = s.tm;
+        p.tn = s.tn;
+        p.mt = (int)ceil_div(rows, s.tm);
+        p.nt = (int)ceil_div(cols, s.tn);
+        p.tiles = sym ? p.mt * (p.mt + 1) / 2 : p.mt * p.nt;
+        const int64_t all = (int64_t)p.tiles * batch, round = (int64_t)kCus * s.resident;
+        auto rounds = [&](int64_t groups) {
+            const int64_t left = groups % round;
+            const double fill = s.resident == 1 ? (double)left / kCus : left > kCus ? 1.0 : 0.0;
+            return (double)(groups / round) * s.full + (left ? s.one + (s.full - s.one) * fill : 0.0);
+        };
+        for (int want = 1; want <= 16; ++want)
+            for (int some = 0; some <= (want > 1 && all > round); ++some) {
+                p.rest = want == 1 ? 0 : some ? all % round : all;
+                p.whole = all - p.rest;
+                p.per = (int)ceil_div(stages, want);
+                p.splits = (int)ceil_div(stages, p.per);
+                if (want > 1 && (p.per < 4 || p.rest == 0)) continue;
+                double t = s.fixed + stages * rounds(p.whole) + p.per * rounds(p.rest * p.splits) + entries * 0.7e-6;
+                if (p.rest > 0) t += 4.8 + 0.26 * p.splits + p.rest * s.tm * s.tn * (0.25e-6 + 1.0e-6 * p.splits) + (some ? 0.5 * s.fixed : 0.0);
+                if (least == 0.0 || t < least) {
+                    least = t;
+                    best = p;
+                }
             }
-        }
+    }
     return best;
 }
 
@@ -541,17 +577,17 @@ size_t carve(int batch, int r, int c, bool split, void *base, Buffers *out) {
     b.t[1] = planes(cp, rp);
     b.a = planes(rp, rp);
     b.b = planes(rp, rp);
-    // fp32 sums of the split products: those of X (r x c) and of A and B
+    // fp32 sums of the split products
     int64_t sums = 0;
     const int passes = split ? 3 : 1;
     auto room = [&](int64_t rows, int64_t cols, int64_t k, bool sym) {
         const ProductPlan p = plan_product(batch, (int)rows, (int)cols, passes * (int)(k / 64), sym);
-        if (p.splits > 1) sums = std::max(sums, p.splits * rows * cols);
+        sums = std::max(sums, p.rest * p.splits * p.tm * p.tn);
     };
     room(rp, rp, cp, true);
     room(rp, rp, rp, true);
     room(rp, cp, rp, false);
-    b.sums = reinterpret_cast<float *>(take(sizeof(float) * (size_t)sums * batch));
+    b.sums = reinterpret_cast<float *>(take(sizeof(float) * (size_t)sums));
     if (out) *out = b;
     return off;
 }
@@ -563,21 +599,22 @@ void launch_product(ProductArgs &g, int batch, hipStream_t st) {
     g.mt = p.mt;
     g.nt = p.nt;
     g.tiles = p.tiles;
+    g.tm = p.tm;
+    g.tn = p.tn;
     g.batch = batch;
+    g.whole = p.whole;
+    g.rest = p.rest;
     g.splits = p.splits;
     g.per = p.per;
-    const int64_t all = (int64_t)p.tiles * batch * p.splits;
-    if (p.size == kPipeTile) {
-        g.chunk = (int)ceil_div(all, kXcds);
-        product_pipe<SPLIT, KIND><<<(unsigned)(kXcds * g.chunk), 256, 0, st>>>(g);
-    } else if (p.size == 128) {
-        product_tile<SPLIT, KIND, 2, 2, 4, 2><<<(unsigned)all, 256, 0, st>>>(g);
-    } else {
-        product_tile<SPLIT, KIND, 4, 1, 1, 4><<<(unsigned)all, 256, 0, st>>>(g);
-    }
-    if (p.splits > 1) {
-        const int mt = g.rows / 64, nt = g.cols / 64;
-        const int64_t blocks = (symmetric(KIND) ? (int64_t)mt * (mt + 1) / 2 : (int64_t)mt * nt) * batch;
+    g.whole_chunk = (int)ceil_div(p.whole, kXcds);
+    g.rest_chunk = (int)ceil_div(p.rest * p.splits, kXcds);
+    const unsigned grid = (unsigned)(kXcds * (g.whole_chunk + g.rest_chunk));
+    if (p.tm == 64) product_tile<SPLIT, KIND, 4, 1, 1, 4><<<grid, 256, 0, st>>>(g);
+    else if (p.tm == 128) product_tile<SPLIT, KIND, 2, 2, 4, 2><<<grid, 256, 0, st>>>(g);
+    else if (p.tn == 256) product_pipe<SPLIT, KIND, 8><<<grid, 256, 0, st>>>(g);
+    else if constexpr (!symmetric(KIND)) product_pipe<SPLIT, KIND, 4><<<grid, 256, 0, st>>>(g);
+    if (p.rest > 0) {
+        const int64_t blocks = p.rest * (p.tm / 32) * (p.tn / 64);
         product_join<SPLIT, KIND><<<(unsigned)blocks, 256, 0, st>>>(g);
     }
 }

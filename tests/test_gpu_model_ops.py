@@ -310,7 +310,9 @@ def test_orthogonalize(o2m, rows, cols, dtype, order):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("batch,rows,cols,order", [(1, 1100, 3900, "row"), (1, 2300, 1400, "col"), (40, 260, 300, "row")])
+@pytest.mark.parametrize("batch,rows,cols,order", [(1, 1100, 3900, "row"), (1, 2300, 1400, "col"), (40, 260, 300, "row"),
+                                                   (16, 900, 1101, "row"), (1, 2000, 5001, "col"), (15, 1000, 1300, "col"),
+                                                   (18, 1000, 1399, "row")])
 def test_orthogonalize_large(o2m, batch, rows, cols, order, dtype):
     """Enough tiles for the kernels of large products, the last ones beside the
     matrix; a step or two, which the bound tells apart from anything else."""
