@@ -593,9 +593,7 @@ size_t carve(int batch, int r, int c, bool split, void *base, Buffers *out) {
 }
 
 template <bool SPLIT, Product KIND>
-void launch_product(ProductArgs &g, int batch, hipStream_t st) {
-    const int stages = (SPLIT ? 3 : 1) * g.kblocks;
-    const ProductPlan p = plan_product(batch, g.rows, g.cols, stages, symmetric(KIND));
+void launch_product(ProductArgs &g, const ProductPlan &p, int batch, hipStream_t st) {
     g.mt = p.mt;
     g.nt = p.nt;
     g.tiles = p.tiles;
@@ -643,7 +641,10 @@ hipError_t run_ortho(const OrthoArgs &o, const Buffers &b, hipStream_t st) {
         write_x<SPLIT><<<dim3(std::min<int64_t>(1024, ceil_div((int64_t)r * c, 256)), o.batch), 256, 0, st>>>(b.x, g);
         return hipGetLastError();
     }
-    const int rp = rt * kPad, cp = ct * kPad;
+    const int rp = rt * kPad, cp = ct * kPad, passes = SPLIT ? 3 : 1;
+    const ProductPlan gram = plan_product(o.batch, rp, rp, passes * ct, true),
+                      poly = plan_product(o.batch, rp, rp, passes * rt, true),
+                      update = plan_product(o.batch, rp, cp, passes * rt, false);
     g.parts = b.sums;
     for (int step = 0; step < o.steps; ++step) {
         const double *k = o.coef + 3 * step;
@@ -653,22 +654,22 @@ hipError_t run_ortho(const OrthoArgs &o, const Buffers &b, hipStream_t st) {
         g.d = g.dt = b.a;
         g.kblocks = cp / 64;
         g.mul = (float)ldexp(1.0, kScaleA - 2 * kScaleX);
-        launch_product<SPLIT, kGram>(g, o.batch, st);
+        launch_product<SPLIT, kGram>(g, gram, o.batch, st);
         g.p = g.q = g.e = b.a;
         g.d = g.dt = b.b;
         g.kblocks = rp / 64;
         g.diag = (float)ldexp(k[0], kScaleB);
         g.add = (float)ldexp(k[1], kScaleB - kScaleA);
         g.mul = (float)ldexp(k[2], kScaleB - 2 * kScaleA);
-        launch_product<SPLIT, kPoly>(g, o.batch, st);
+        launch_product<SPLIT, kPoly>(g, poly, o.batch, st);
         g.p = b.b;
         g.q = t;
         g.d = b.x;
         g.dt = t_next;
         g.cols = cp;
         g.mul = (float)ldexp(1.0, -kScaleB);
-        if (step + 1 < o.steps) launch_product<SPLIT, kUpdate>(g, o.batch, st);
-        else launch_product<SPLIT, kLast>(g, o.batch, st);
+        if (step + 1 < o.steps) launch_product<SPLIT, kUpdate>(g, update, o.batch, st);
+        else launch_product<SPLIT, kLast>(g, update, o.batch, st);
     }
     return hipGetLastError();
 }
