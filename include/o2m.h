@@ -312,7 +312,7 @@ typedef struct {
    (s = 1 when amax = 0), and an entry becomes fl(x fl(1/s)), limited to
    [-F, F] and rounded to the nearest 8-bit number, ties to even; Inf and NaN
    become NaN.  The blocks at the edges are shorter, nothing is written past
-   them.  Argument errors: -1 rows, -2 k, -3 X, -4 x_type, -5 x_order, -6 ldx,
+   them.  The scales of an operand have to lie apart, and Q and Qt too.  Argument errors: -1 rows, -2 k, -3 X, -4 x_type, -5 x_order, -6 ldx,
    -7 Q, -8 Qt. */
 o2m_status o2m_quantize_fp8(int rows, int k, const void *X, int x_type, char x_order, int64_t ldx,
                             const o2m_fp8_operand *Q, const o2m_fp8_operand *Qt, void *stream);
@@ -322,9 +322,10 @@ o2m_status o2m_quantize_fp8(int rows, int k, const void *X, int x_type, char x_o
    fp32 results the products are exact and summed in fp32.  For 16-bit ones they are
    summed by the 8-bit matrix unit, which adds 8 neighbouring products (k = 8 t
    .. 8 t + 7) to within 2^-13 of the largest of them each, and these sums in
-   fp32: some 2e-5 of the result's norm, far below its rounding.  accumulate != 0: C += A B^T, the sum rounded once.  c_order 'R':
-   entry (i, j) at C[i ldc + j], 'C': at C[i + j ldc].  Rows holding NaN give
-   NaN.  k == 0: C is set to zero (accumulate: left as it is).  Every run
+   fp32: some 2e-5 of the result's norm, far below its rounding.  The products of
+   two blocks' scales, and sums, have to stay within fp32's range.  accumulate !=
+   0: C += A B^T, the sum rounded once.  c_order 'R': entry (i, j) at C[i ldc + j],
+   'C': at C[i + j ldc].  Rows holding NaN give NaN.  k == 0: C is set to zero (accumulate: left as it is).  Every run
    gives the same bits.  Argument errors: -1 m, -2 n, -3 k, -4 A, -5 B, -6 C,
    -7 c_type, -8 c_order, -9 ldc. */
 o2m_status o2m_gemm_fp8(int m, int n, int k, const o2m_fp8_operand *A, const o2m_fp8_operand *B, void *C,
@@ -354,8 +355,8 @@ size_t o2m_linear_fp8_workspace(int tokens, int n, int k);
    result), fp32 and fp16 ones in two fp16 parts (22 bits).  The held range
    asks for singular values below 4 in every step, which the usual
    coefficients keep far below 2.  A matrix has at most 2^29 entries (its sizes
-   rounded up to multiples of 64) and a side of at most 2^21.  Inf or NaN in G gives NaN in the whole
-   matrix.  O must not overlap G, except to be G in the same layout.  Argument
+   rounded up to multiples of 64) and a side of at most 2^21.  Inf or NaN in G
+   gives NaN in the whole matrix.  O must not overlap G, except to be G in the same layout.  Argument
    errors: -1 batch, -2 rows, -3 cols, -4 G, -5 order_g, -6 ldg, -7 stride_g,
    -8 O, -9 order_o, -10 ldo, -11 stride_o, -12 type, O2M_ERR_STEPS steps,
    coef or eps. */

@@ -35,6 +35,16 @@ bool operand_ok(const o2m_fp8_operand *o, int k) {
            (o->scale_type == O2M_SCALES_POW2 || (o->scale_type == O2M_SCALES_F32 && aligned(o->scales, 4)));
 }
 
+// Scales to be written have a place each.
+bool scales_apart(const o2m_fp8_operand *o, int rows, int k) {
+    const int64_t r = o->block == 1 ? rows : ceil_div(rows, kBlockK), b = ceil_div(k, kBlockK);
+    return (r == 1 || o->s_row >= 1) && (b == 1 || o->s_blk >= 1) &&
+           (r == 1 || b == 1 || o->s_row > (b - 1) * o->s_blk || o->s_blk > (r - 1) * o->s_row);
+}
+
+// Sizes up to here, so that a row past the last tile is still an int.
+constexpr int kMaxSize = 0x7FFFFFFF - 1023;
+
 o2m_status check_workspace(size_t need, const void *ws, size_t bytes) {
     if (need == 0) return O2M_OK;
     return ws && bytes >= need && aligned(ws, 256) ? O2M_OK : O2M_ERR_WORKSPACE;
@@ -75,8 +85,10 @@ o2m_status o2m_quantize_fp8(int rows, int k, const void *X, int x_type, char x_o
     if (ldx < (order == 'R' ? k : rows) || ldx < 1) return -6;
     if (!Q && !Qt) return -7;
     if (!any) return O2M_OK;
-    if (Q && !operand_ok(Q, k)) return -7;
-    if (Qt && !operand_ok(Qt, rows)) return -8;
+    if (Q && (!operand_ok(Q, k) || !scales_apart(Q, rows, k))) return -7;
+    if (Qt && (!operand_ok(Qt, rows) || !scales_apart(Qt, k, rows))) return -8;
+    if (Q && Qt && (Q->values == Qt->values || Q->scales == Qt->scales)) return -8;
+    if (rows > kMaxSize || k > kMaxSize) return O2M_ERR_SIZE;
     const hipStream_t st = (hipStream_t)stream;
     return hip_fail(order == 'R' ? launch_quantize(rows, k, X, x_type, ldx, Q, Qt, st)
                                  : launch_quantize(k, rows, X, x_type, ldx, Qt, Q, st));
@@ -108,7 +120,7 @@ o2m_status o2m_gemm_fp8(int m, int n, int k, const o2m_fp8_operand *A, const o2m
         if (accumulate) return O2M_OK;
         return hip_fail(launch_zero_out(C, swap ? m : n, swap ? n : m, ldc, type_bytes(c_type), st));
     }
-    if (A->ld >= kMaxPitch || B->ld >= kMaxPitch) return O2M_ERR_SIZE;
+    if (A->ld >= kMaxPitch || B->ld >= kMaxPitch || m > kMaxSize || n > kMaxSize) return O2M_ERR_SIZE;
     const o2m_status s = check_workspace(gemm_fp8_workspace(m, n, k), workspace, workspace_bytes);
     if (s != O2M_OK) return s;
     return hip_fail(swap ? launch_gemm_fp8(n, m, k, *B, *A, C, c_type, ldc, accumulate != 0, workspace, st)
@@ -136,7 +148,7 @@ o2m_status o2m_linear_fp8(int tokens, int n, int k, const void *X, int x_type, i
     if (!any) return O2M_OK;
     const hipStream_t st = (hipStream_t)stream;
     if (k == 0) return hip_fail(launch_zero_out(Y, n, tokens, ldy, type_bytes(x_type), st));
-    if (W->ld >= kMaxPitch || round_up64(k, 16) >= kMaxPitch) return O2M_ERR_SIZE;
+    if (W->ld >= kMaxPitch || round_up64(k, 16) >= kMaxPitch || tokens > kMaxSize || n > kMaxSize) return O2M_ERR_SIZE;
     const o2m_status s = check_workspace(o2m_linear_fp8_workspace(tokens, n, k), workspace, workspace_bytes);
     if (s != O2M_OK) return s;
     if (linear_is_fused(tokens, k)) return hip_fail(launch_linear_fused(tokens, n, k, X, x_type, ldx, *W, Y, ldy, st));

@@ -9,9 +9,11 @@
 // that matters), which costs nothing here.  The waves' sums are joined in LDS in a
 // fixed order.
 //
-// One or two tokens are quantized by each workgroup for itself: reading the
-// tokens again is some 2% of reading W, and a launch of its own would cost as
-// much as 20 MB of W.
+// Tokens of up to 16 KB in 8 bits (two of 8192 entries, 16 of 1024) are quantized by
+// each workgroup for itself: reading them again is some 2% of reading W a token,
+// from the cache, and a launch of its own would cost as much as 20 MB of W.
+//
+// 1 x 8192 x 8192 16.2 us (67 MB at 4.1 TB/s; a large copy moves 4.9).
 #include "fp8_operand.h"
 #include "fp8_round.h"
 

@@ -84,12 +84,14 @@ def _type_of(x: torch.Tensor, name: str) -> int:
 
 def _order(rows: int, cols: int, s0: int, s1: int, name: str):
     """(order, leading dimension) of a rows x cols matrix with these strides."""
-    if rows <= 1 or cols <= 1 or rows * cols == 0:
-        if rows * cols == 0 or (cols <= 1 and rows <= 1):
+    if rows <= 1 or cols <= 1:
+        if rows * cols <= 1:
             return b"R", max(cols, 1)
+        if (s0 if cols == 1 else s1) < 1:
+            raise ValueError(f"{name} must hold its entries apart from one another (strides of 1 and more)")
         if cols == 1:
-            return b"R", max(s0, 1)              # entry i at i s0
-        return (b"R", cols) if s1 == 1 else (b"C", max(s1, 1))
+            return b"R", s0                      # entry i at i s0
+        return (b"R", cols) if s1 == 1 else (b"C", s1)
     if s1 == 1:
         return b"R", s0
     if s0 == 1:

@@ -183,6 +183,31 @@ def test_gemm_out(o2m, scales, dtype):
             assert (buf == 7.0).all()
 
 
+@pytest.mark.parametrize("m,n,k", [(5, 90, 300), (70, 90, 300), (1900, 2100, 1000), (3700, 3600, 400)])
+@pytest.mark.parametrize("scales", ["pow2", "float32"])
+def test_gemm_orders_of_scales(o2m, m, n, k, scales):
+    """Scales in either order, as bytes, or one for all blocks (strides of 0): the
+    same values, so the same product; sizes for the kernels of each tile."""
+    a, b = matrix(m, k, 6, spread=0.5), matrix(n, k, 7, spread=0.5)
+    A, B = o2m.quantize_fp8(a, scales=scales), o2m.quantize_fp8(b, (128, 128), scales=scales)
+    want = o2m.gemm_fp8(A, B)
+    R.check_product(want, R.values64(A, 1), R.values64(B, 128), torch.bfloat16)
+    wide = torch.empty((m, 2 * A.scales.size(1)), dtype=A.scales.dtype, device=DEV)[:, ::2]
+    wide.copy_(A.scales)
+    for s in (A.scales.contiguous(), wide, A.scales.t().contiguous().t()):
+        for t in (B.scales.contiguous(), B.scales.t().contiguous().t()):
+            R.check_product(o2m.gemm_fp8((A.values, s), (B.values, t)), R.values64(A, 1), R.values64(B, 128), torch.bfloat16)
+            if scales == "pow2":
+                assert torch.equal(o2m.gemm_fp8((A.values, s), (B.values, t)),
+                                   o2m.gemm_fp8((A.values, s.view(torch.uint8)), (B.values, t.view(torch.uint8))))
+    one = torch.full((1, 1), 0.5, device=DEV).to(A.scales.dtype)
+    s, t = one.expand(m, A.scales.size(1)), one.expand(B.scales.shape)
+    full = o2m.gemm_fp8((A.values, s.contiguous()), (B.values, t.contiguous()), dtype=torch.float32)
+    assert torch.equal(o2m.gemm_fp8((A.values, s), (B.values, t), dtype=torch.float32), full)
+    R.check_product(full, R.values64(o2m.Fp8Operand(A.values, s), 1), R.values64(o2m.Fp8Operand(B.values, t), 128),
+                    torch.float32)
+
+
 def test_gemm_non_finite_rows(o2m):
     m, n, k = 40, 50, 200
     for scales in ("pow2", "float32"):

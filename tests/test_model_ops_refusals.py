@@ -47,6 +47,30 @@ def test_quantize_refuses_operands(bad):
     assert quantize(rows=40, Qt=operand(**bad)) == -8
 
 
+@pytest.mark.parametrize("bad", [dict(s_row=0), dict(s_blk=0), dict(s_row=1, s_blk=7), dict(s_row=2, s_blk=2),
+                                 dict(s_row=0, block=128), dict(s_blk=0, block=128), dict(s_row=2, s_blk=2, block=128)])
+def test_quantize_refuses_scales_on_one_another(bad):
+    """300 x 300 entries: 300 or 3 by 3 scales."""
+    q = operand(ld=304, **{**dict(s_blk=300), **bad})
+    other = operand(ld=304, values=2 * PTR, scales=2 * PTR, s_blk=300)
+    assert quantize(300, 300, ld=300, Q=q) == -7
+    assert quantize(300, 300, ld=300, Q=other, Qt=q) == -8
+
+
+def test_quantize_refuses_one_operand_for_both():
+    q = operand(ld=304, s_blk=300)
+    for same in (dict(values=PTR, scales=2 * PTR), dict(values=2 * PTR, scales=PTR)):
+        assert quantize(300, 300, ld=300, Q=q, Qt=operand(ld=304, s_blk=300, **same)) == -8
+
+
+def test_sizes_past_the_last_tile():
+    n, far = (1 << 31) - 1, operand(ld=1 << 31, s_row=1, s_blk=1 << 31)
+    assert quantize(n, 40, ld=64, Q=operand(s_blk=n)) == SIZE
+    assert quantize(8, n, ld=n, Q=far) == SIZE
+    assert gemm(m=n) == SIZE and gemm(n=n, ld=n) == SIZE
+    assert linear(tokens=n) == SIZE and linear(n=n, ldy=n) == SIZE
+
+
 def gemm(m=8, n=9, k=40, A=None, B=None, C=PTR, t=2, order=b"R", ld=64, add=0):
     a, b = A or operand(), B or operand()
     return L.o2m_gemm_fp8(m, n, k, ctypes.byref(a), ctypes.byref(b), C, t, order, ld, add, None, 0, None)
@@ -149,3 +173,9 @@ def test_binding_refuses():
                  lambda: o2m.orthogonalize(torch.zeros(5)), lambda: o2m.quantize_fp8_pair(torch.zeros(5))):
         with pytest.raises(ValueError):
             call()
+    # entries that all lie in one place, of a single row or column
+    for rows, cols, s0, s1 in ((1, 5, 0, 0), (5, 1, 0, 1), (5, 1, 0, 0), (1, 5, 1, 0)):
+        with pytest.raises(ValueError):
+            M._order(rows, cols, s0, s1, "X")
+    assert M._order(1, 5, 0, 2, "X") == (b"C", 2) and M._order(5, 1, 3, 0, "X") == (b"R", 3)
+    assert M._order(1, 1, 0, 0, "X") == (b"R", 1) and M._order(0, 7, 0, 0, "X") == (b"R", 7)
