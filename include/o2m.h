@@ -322,8 +322,9 @@ o2m_status o2m_quantize_fp8(int rows, int k, const void *X, int x_type, char x_o
    fp32 results the products are exact and summed in fp32.  For 16-bit ones they are
    summed by the 8-bit matrix unit, which adds 8 neighbouring products (k = 8 t
    .. 8 t + 7) to within 2^-13 of the largest of them each, and these sums in
-   fp32: some 2e-5 of the result's norm, far below its rounding.  The products of
-   two blocks' scales, and sums, have to stay within fp32's range.  accumulate !=
+   fp32: some 2e-5 of the result's norm, far below its rounding.  Scaled
+   entries, the products of two blocks' scales, and sums have to stay within the
+   range of normal fp32 numbers (smaller ones may count as zeros).  accumulate !=
    0: C += A B^T, the sum rounded once.  c_order 'R': entry (i, j) at C[i ldc + j],
    'C': at C[i + j ldc].  Rows holding NaN give NaN.  k == 0: C is set to zero (accumulate: left as it is).  Every run
    gives the same bits.  Argument errors: -1 m, -2 n, -3 k, -4 A, -5 B, -6 C,

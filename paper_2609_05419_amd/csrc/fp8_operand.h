@@ -22,6 +22,8 @@ struct Side {
 
 typedef _Float16 v2f16 __attribute__((ext_vector_type(2)));
 typedef _Float16 v8f16 __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf16 __attribute__((ext_vector_type(2)));
+typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
 
 // Eight 8-bit values (two dwords) in fp16, exactly.
 template <int F>
@@ -36,6 +38,22 @@ __device__ inline v8f16 widen(int x, int y) {
                                          : __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w[i], 1.0f, true);
     }
     return v8f16{r[0][0], r[0][1], r[1][0], r[1][1], r[2][0], r[2][1], r[3][0], r[3][1]};
+}
+
+// The same with a power-of-two scale, in bf16: exactly where the products lie within
+// its normal range.
+template <int F>
+__device__ inline v8bf16 widen_scaled(int x, int y, float scale) {
+    v2bf16 r[4];
+    const uint32_t w[2] = {(uint32_t)x, (uint32_t)y};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        r[2 * i] = F == O2M_FP8_E4M3 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false)
+                                     : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i], scale, false);
+        r[2 * i + 1] = F == O2M_FP8_E4M3 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true)
+                                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i], scale, true);
+    }
+    return v8bf16{r[0][0], r[0][1], r[1][0], r[1][1], r[2][0], r[2][1], r[3][0], r[3][1]};
 }
 
 __device__ inline float load_out(const void *C, int64_t i, int type) {

@@ -10,9 +10,10 @@ namespace o2m {
 
 // How a block's products are added up.
 enum Sum {
-    kScaled,    // 8-bit MFMA with power-of-two scales
-    kPartial,   // 8-bit MFMA, then fp32 scales
-    kWide,      // fp16 MFMA, then scales of either kind
+    kScaled,       // 8-bit MFMA with power-of-two scales
+    kPartial,      // 8-bit MFMA, then fp32 scales
+    kWide,         // fp16 MFMA, then fp32 scales
+    kWideScaled,   // bf16 MFMA of values scaled by powers of two as they are widened
 };
 
 // C = A B^T, entry (i, j) at C[i ldc + j].
@@ -26,8 +27,6 @@ struct Fp8Args {
     float *parts;        // split launches: sums [split][m][pitch]
     int pitch, splits, per;
 };
-
-typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
 
 // N (4 or 8) neighbouring outputs of a row, from `col` on, at once where all exist.
 // (The accesses need no alignment but the entries' own.)
@@ -144,7 +143,7 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
         uint8_t *buf = lds + u * T::kBuf;
         const int left = g.k - kb * kBlockK;
         if (tid < T::kRows)
-            scales[(kb & 1) * T::kRows + tid] = SUM == kWide && side.pow2 ? __float_as_uint(code_value(ahead[a])) : ahead[a];
+            scales[(kb & 1) * T::kRows + tid] = SUM == kWideScaled ? __float_as_uint(code_value(ahead[a])) : ahead[a];
         // this stage has landed; those after it, if there are S - 2, need not
         if (S > 2 && kb + S - 1 <= s1) wait_vmem<(S > 2 ? S - 2 : 0) * T::kIssues>();
         else wait_vmem<0>();
@@ -163,12 +162,17 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
         v8i fb[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) fb[j] = read_fragment<2>(buf + T::kTm * kStageRowBytes, wj + 4 * q + j, lane);
-        v8f16 wb[SUM == kWide ? 4 : 1][4];
+        std::conditional_t<SUM == kWideScaled, v8bf16, v8f16> wb[SUM >= kWide ? 4 : 1][4];
         if constexpr (SUM == kWide) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int h = 0; h < 4; ++h) wb[j][h] = widen<FB>(fb[j][2 * h], fb[j][2 * h + 1]);
+        } else if constexpr (SUM == kWideScaled) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int h = 0; h < 4; ++h) wb[j][h] = widen_scaled<FB>(fb[j][2 * h], fb[j][2 * h + 1], sb[j]);
         }
 #pragma unroll
         for (int i = 0; i < M; ++i) {
@@ -179,6 +183,15 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
                 for (int j = 0; j < 4; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
                         fa, fb[j], acc[i][j], FA, FB, 0, ca, 0, cb[j]);
+            } else if constexpr (SUM == kWideScaled) {
+                const float sa = __uint_as_float(sc[wi + 16 * i + q]);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const v8bf16 wa = widen_scaled<FA>(fa[2 * h], fa[2 * h + 1], sa);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, wb[j][h], acc[i][j], 0, 0, 0);
+                }
             } else {
                 v4f sa = *reinterpret_cast<const v4f *>(sc + wi + 16 * i + 4 * (lane >> 4));
                 if (WB) sa *= sb[0];

@@ -12,10 +12,13 @@
 // below 2^-24).  On normal data in blocks a sum is 1.5e-5 to 3e-5 off in the
 // 2-norm: far below the rounding of a bf16 (1.7e-3) or fp16 (2.1e-4) result,
 // which therefore take it, and far above that of an fp32 one.  Products with an
-// fp32 result turn the values to fp16 in registers, which holds both formats
-// exactly, and add up with v_mfma_f32_16x16x32_f16 (6e-8), at half the rate.
+// fp32 result turn the values to 16 bits in registers and add up with
+// v_mfma_f32_16x16x32 (6e-8), at half the rate: to fp16, which holds both formats
+// exactly, and scale a block's sum, or, where scales are powers of two, to bf16
+// times the scale, which is exact as well and leaves nothing to do after the
+// MFMAs (4096^3 140 -> 124 us).
 //
-// Bound: 8-bit (fp32 results: fp16) MFMA for large products.
+// Bound: 8-bit (fp32 results: 16-bit) MFMA for large products.
 //
 // Which kernel runs (plan_fp8):
 //   up to 32 rows on one side          k_fp8_few.hip, bound by reading the other
@@ -56,7 +59,7 @@ constexpr int kFewRows = 32;
 // workgroups after the other.  A size has `fixed` per round (its first copies and
 // its results), and per stage `one` while a CU has one workgroup, `full` with all
 // of `resident` (of one resident: while few CUs work, and when all do, which
-// lowers the clock).  Fitted to 37 products of 13 shapes, of which the measured
+// lowers the clock).  Fitted to 50 products of 14 shapes, of which the measured
 // best or one within 3% of it is taken but for 1537 x 1283 x 2051, whose rows of odd
 // lengths cost more (8%).  Measured (us; tiles of 256 x 256, 256 x 128, 128 x 128,
 // 64 x 64):
@@ -67,8 +70,9 @@ constexpr int kFewRows = 32;
 //                            1000 x 1000 x 1000     22    16    11     7
 //   fp32 scales              4096 x 4096 x 4096     75          86   143
 //                            2048 x 4096 x 8192    124          87   136
-//   fp32 results             4096 x 4096 x 4096                140   222
+//   fp32 scales and results  4096 x 4096 x 4096                140   222
 //                            512 x 2048 x 2048                  25    15
+//   powers of two, fp32 res. 4096 x 4096 x 4096                127   211
 // (fp32 results: the widened fragments leave no registers for tiles of 256 x 256,
 // which took 151 us with spilled ones.)  Tiles of 64 x 64 that leave CUs idle are
 // split along k, from 4 stages each: 300 x 300 x 8000 (25 tiles) 30 us in one piece,
@@ -84,11 +88,12 @@ struct TileCost {
     int rows, cols, resident;
     double fixed, one, full;
 };
-constexpr TileCost kCosts[3][4] = {
+constexpr TileCost kCosts[4][4] = {
     {{k256, 256, 256, 1, 13.0, 1.00, 1.33}, {k256x128, 256, 128, 1, 9.5, 0.69, 0.82},
      {k128, 128, 128, 2, 6.5, 0.70, 1.03}, {k64, 64, 64, 2, 3.5, 0.37, 0.45}},
     {{k256, 256, 256, 1, 11.0, 1.70, 2.00}, {}, {k128, 128, 128, 2, 6.5, 0.84, 1.24}, {k64, 64, 64, 2, 3.7, 0.42, 0.51}},
-    {{}, {}, {k128, 128, 128, 2, 8.0, 1.22, 1.98}, {k64, 64, 64, 2, 4.2, 0.66, 0.82}}};
+    {{}, {}, {k128, 128, 128, 2, 8.0, 1.22, 1.98}, {k64, 64, 64, 2, 4.2, 0.66, 0.82}},
+    {{}, {}, {k128, 128, 128, 2, 7.5, 1.15, 1.80}, {k64, 64, 64, 2, 4.0, 0.60, 0.79}}};
 
 Plan plan_fp8(int m, int n, int k, Sum sum) {
     const int kblocks = (int)ceil_div(k, kBlockK);
@@ -137,7 +142,7 @@ hipError_t launch_zero_out(void *C, int64_t m, int64_t n, int64_t ldc, int size,
 size_t gemm_fp8_workspace(int m, int n, int k) {
     // either order of the result: its rows are those of one operand or the other
     int splits = 1;
-    for (const Sum sum : {kScaled, kPartial, kWide})
+    for (const Sum sum : {kScaled, kPartial, kWide, kWideScaled})
         splits = std::max({splits, plan_fp8(m, n, k, sum).splits, plan_fp8(n, m, k, sum).splits});
     if (splits == 1) return 0;
     return sizeof(float) * (size_t)splits * (size_t)std::max(m * round_up64(n, 4), n * round_up64(m, 4));
@@ -145,7 +150,8 @@ size_t gemm_fp8_workspace(int m, int n, int k) {
 
 hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const o2m_fp8_operand &B, void *C, int type,
                            int64_t ldc, bool accumulate, void *ws, hipStream_t st) {
-    const Plan p = plan_fp8(m, n, k, type == O2M_TYPE_F32 ? kWide : A.scale_type == O2M_SCALES_POW2 ? kScaled : kPartial);
+    const bool wide = type == O2M_TYPE_F32;
+    const Plan p = plan_fp8(m, n, k, A.scale_type == O2M_SCALES_POW2 ? (wide ? kWideScaled : kScaled) : wide ? kWide : kPartial);
     if (p.few)
         return n <= m ? launch_few(n, m, k, B, A, C, type, 1, ldc, accumulate, st)
                       : launch_few(m, n, k, A, B, C, type, ldc, 1, accumulate, st);
@@ -166,9 +172,9 @@ hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const 
     // the large kernel of power-of-two scales reads those of 8 rows at once
     auto fits = [](const Side &s) { return !s.by_row || (s.s_row == 1 && s.rows >= 8); };
     const TileSize size = p.size <= k256x128 && g.a.pow2 && !(fits(g.a) && fits(g.b)) ? k128 : p.size;
-    const hipError_t e = type == O2M_TYPE_F32 ? launch_fp8_wide(g, format, size, st)
-                         : g.a.pow2           ? launch_fp8_scaled(g, format, size, st)
-                                              : launch_fp8_partial(g, format, size, st);
+    const hipError_t e = wide       ? launch_fp8_wide(g, format, size, st)
+                         : g.a.pow2 ? launch_fp8_scaled(g, format, size, st)
+                                    : launch_fp8_partial(g, format, size, st);
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t threads = (int64_t)m * (g.pitch / 4);
     join_parts<<<(unsigned)std::min<int64_t>(ceil_div(threads, 256), 2048), 256, 0, st>>>(g);

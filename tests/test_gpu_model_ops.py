@@ -208,6 +208,25 @@ def test_gemm_orders_of_scales(o2m, m, n, k, scales):
                     torch.float32)
 
 
+def test_gemm_ends_of_the_scales(o2m):
+    """Scales that are NaN, and the smallest and largest that leave scaled entries
+    normal, against ones of the other end."""
+    m, n, k = 300, 260, 384
+    a, b = matrix(m, k, 8, spread=0.5), matrix(n, k, 9, spread=0.5)
+    A, B = o2m.quantize_fp8(a), o2m.quantize_fp8(b, (128, 128))
+    low, high = o2m.Fp8Operand(A.values, torch.full_like(A.scales.view(torch.uint8), 127 - 110)), o2m.Fp8Operand(
+        B.values, torch.full_like(B.scales.view(torch.uint8), 127 + 110))
+    for dtype in TYPES:
+        want = R.values64(o2m.Fp8Operand(A.values, torch.ones_like(A.scales, dtype=torch.float32)), 1)
+        other = R.values64(o2m.Fp8Operand(B.values, torch.ones_like(B.scales, dtype=torch.float32)), 128)
+        if dtype != torch.float16:   # (beyond fp16's range)
+            R.check_product(o2m.gemm_fp8(low, high, dtype=dtype), want, other, dtype)
+        s = A.scales.view(torch.uint8).clone()
+        s[37, 1] = 255
+        C = o2m.gemm_fp8(o2m.Fp8Operand(A.values, s), B, dtype=dtype)
+        assert torch.isnan(C[37]).all() and torch.isfinite(C[:37]).all() and torch.isfinite(C[38:]).all()
+
+
 def test_gemm_non_finite_rows(o2m):
     m, n, k = 40, 50, 200
     for scales in ("pow2", "float32"):
