@@ -5,7 +5,8 @@
 // Bound: latency.  Each product is one round of the waves, a wave owning 32 x 32 of
 // its outputs (2 x 2 blocks of 16 x 16), between barriers; 15 of them for five
 // steps, where separate launches take 3 us and more each (16 matrices of 96 x 80
-// in fp32: 105 us in 17 launches).
+// in fp32: 43 us, of them 14 to load and write and 5.8 a step, against 105 in 17
+// launches).
 #include "ortho_shared.h"
 
 #include <math.h>
