@@ -72,28 +72,27 @@ __device__ inline void store_run(const Fp8Args &g, int row, int col, V v) {
         if (j < n) store_out(g.C, at + j, g.type, v[j] + (g.accumulate ? load_out(g.C, at + j, g.type) : 0.0f));
 }
 
-// WR x WC waves of M x 4 blocks of 16 x 16 and a ring of S stage buffers.  Rows of a
+// WR x WC waves of M x 4 blocks of 16 x 16 and two stage buffers.  Rows of a
 // wave are 16 i + q (block i, q = lane % 16), columns 4 q + j, so that a lane's
 // blocks j are neighbouring columns.  WB: B's scale is one for the wave's columns.
-template <int WR, int WC, int M, int S>
+template <int WR, int WC, int M>
 struct TileOf {
     static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
     static constexpr int kTm = WR * M * 16, kTn = WC * 64, kRows = kTm + kTn;
     static constexpr int kCopyA = kTm / 8 / kWaves, kCopyB = kTn / 8 / kWaves;
     static constexpr int kBuf = kRows * kStageRowBytes;
-    static constexpr int kIssues = kCopyA + kCopyB + 1;   // vector-memory instructions of a stage: copies, a scale
     static_assert(kRows <= kThreads && kCopyA * 8 * kWaves == kTm && kCopyB * 8 * kWaves == kTn, "shares of a stage");
-    static_assert((S - 2) * kIssues <= 63, "what a wait can count");
 };
 
-// Stage kb lies in buffer (kb - s0) % S, and S - 1 stages ahead are on their way.
-// Each thread fetches the scale of one row of A or B as far ahead, into a
-// register, and passes it on in LDS when the stage begins.
-template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M, int S, int OCC>
+// Stage kb lies in buffer (kb - s0) % 2, and the next one is on its way.  Each thread
+// fetches the scale of one row of A or B as far ahead, into a register, and passes
+// it on in LDS when the stage begins.  What hides the latencies of a stage are the
+// OCC workgroups that a CU holds.
+template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M, int OCC>
 __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
-    typedef TileOf<WR, WC, M, S> T;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[S * T::kBuf + 2 * T::kRows * 4];
-    uint32_t *const scales = reinterpret_cast<uint32_t *>(lds + S * T::kBuf);   // [2][A's rows, B's rows]
+    typedef TileOf<WR, WC, M> T;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * T::kBuf + 2 * T::kRows * 4];
+    uint32_t *const scales = reinterpret_cast<uint32_t *>(lds + 2 * T::kBuf);   // [2][A's rows, B's rows]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int z = blockIdx.x % g.splits, slot = blockIdx.x / g.splits;
     const TileCoord tc = tile_of(slot & 7, slot >> 3, g.mt, g.nt, g.chunk, 0);
@@ -130,31 +129,23 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
     for (int i = 0; i < M; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = v4f{0, 0, 0, 0};
-    uint32_t ahead[S == 2 ? 1 : S];
-#pragma unroll
-    for (int u = 0; u < S - 1; ++u)
-        if (s0 + u < s1) {
-            ahead[u] = fetch(s0 + u);
-            copy(s0 + u, lds + u * T::kBuf);
-        }
-    // u = (kb - s0) % S; a: where its scale is; a constant for S > 2
-    auto stage = [&](int kb, int u, auto A) {
-        constexpr int a = A, a_next = S == 2 ? 0 : (a + S - 1) % S;
+    uint32_t ahead = fetch(s0);
+    copy(s0, lds);
+    for (int kb = s0; kb < s1; ++kb) {
+        const int u = (kb - s0) & 1;
         uint8_t *buf = lds + u * T::kBuf;
         const int left = g.k - kb * kBlockK;
         if (tid < T::kRows)
-            scales[(kb & 1) * T::kRows + tid] = SUM == kWideScaled ? __float_as_uint(code_value(ahead[a])) : ahead[a];
-        // this stage has landed; those after it, if there are S - 2, need not
-        if (S > 2 && kb + S - 1 <= s1) wait_vmem<(S > 2 ? S - 2 : 0) * T::kIssues>();
-        else wait_vmem<0>();
+            scales[(kb & 1) * T::kRows + tid] = SUM == kWideScaled ? __float_as_uint(code_value(ahead)) : ahead;
+        wait_vmem<0>();   // this stage has landed
         lds_barrier();
         if (left < kBlockK && (left & 15)) {   // uniform: the last stage of an odd k
             if (tid < T::kRows) clear_row_tail(buf, tid, left, mine_a ? 1 : 2);
             lds_barrier();
         }
-        if (kb + S - 1 < s1) {
-            ahead[a_next] = fetch(kb + S - 1);
-            copy(kb + S - 1, lds + (u + S - 1) % S * T::kBuf);
+        if (kb + 1 < s1) {
+            ahead = fetch(kb + 1);
+            copy(kb + 1, lds + (u ^ 1) * T::kBuf);
         }
         const uint32_t *sc = scales + (kb & 1) * T::kRows;
         const v4i cb = *reinterpret_cast<const v4i *>(sc + T::kTm + wj + 4 * q);   // codes, or floats' bits
@@ -221,14 +212,6 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
                         acc[i][j][e] = fmaf(p[j][e], WB ? sa[e] : sa[e] * sb[j], acc[i][j][e]);
             }
         }
-    };
-    if constexpr (S == 2) {
-        for (int kb = s0; kb < s1; ++kb) stage(kb, (kb - s0) & 1, std::integral_constant<int, 0>());
-    } else {
-        for (int kb = s0; kb < s1; kb += S)
-            each<S>([&](auto U) {
-                if (kb + U < s1) stage(kb + U, U, U);
-            });
     }
 #pragma unroll
     for (int i = 0; i < M; ++i)
@@ -242,30 +225,31 @@ __global__ __launch_bounds__(64 * WR * WC, OCC) void fp8_tile(Fp8Args g) {
         }
 }
 
-template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M, int S, int OCC>
+template <Sum SUM, int FA, int FB, bool WB, int WR, int WC, int M, int OCC>
 hipError_t launch_tile(Fp8Args &g, hipStream_t st) {
-    typedef TileOf<WR, WC, M, S> T;
+    typedef TileOf<WR, WC, M> T;
     g.mt = (int)ceil_div(g.a.rows, T::kTm);
     g.nt = (int)ceil_div(g.b.rows, T::kTn);
     const int64_t chunk = ceil_div((int64_t)g.mt * g.nt, kXcds), grid = kXcds * chunk * g.splits;
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
     g.chunk = (int)chunk;
-    fp8_tile<SUM, FA, FB, WB, WR, WC, M, S, OCC><<<(unsigned)grid, T::kThreads, 0, st>>>(g);
+    fp8_tile<SUM, FA, FB, WB, WR, WC, M, OCC><<<(unsigned)grid, T::kThreads, 0, st>>>(g);
     return hipGetLastError();
 }
 
 // Tile sizes: 256 x 256 by 8 waves (kPartial; kScaled has kernels of its own for this
-// and 256 x 128), 128 x 128 by 4 (two workgroups per CU), 64 x 64 by 4 (two, with twice the stages on
-// their way).
+// and 256 x 128), 128 x 128 by 4 (two workgroups per CU), 64 x 64 by 4 (four; two with
+// three stages on their way each were never faster: 1537 x 1283 x 2051, 525 tiles, 22
+// against 17 us).
 enum TileSize { k256, k256x128, k128, k64 };
 template <Sum SUM, int FA, int FB, bool WB>
 hipError_t launch_sizes(Fp8Args &g, TileSize size, hipStream_t st) {
     switch (size) {
-    case k64: return launch_tile<SUM, FA, FB, WB, 4, 1, 1, 4, 2>(g, st);
-    case k128: return launch_tile<SUM, FA, FB, WB, 2, 2, 4, 2, 2>(g, st);
+    case k64: return launch_tile<SUM, FA, FB, WB, 4, 1, 1, 4>(g, st);
+    case k128: return launch_tile<SUM, FA, FB, WB, 2, 2, 4, 2>(g, st);
     default: break;
     }
-    if constexpr (SUM == kPartial) return launch_tile<SUM, FA, FB, WB, 2, 4, 8, 2, 2>(g, st);
+    if constexpr (SUM == kPartial) return launch_tile<SUM, FA, FB, WB, 2, 4, 8, 2>(g, st);
     return hipErrorInvalidValue;
 }
 

@@ -59,20 +59,21 @@ constexpr int kFewRows = 32;
 // workgroups after the other.  A size has `fixed` per round (its first copies and
 // its results), and per stage `one` while a CU has one workgroup, `full` with all
 // of `resident` (of one resident: while few CUs work, and when all do, which
-// lowers the clock).  Fitted to 50 products of 14 shapes, of which the measured
-// best or one within 3% of it is taken but for 1537 x 1283 x 2051, whose rows of odd
-// lengths cost more (8%).  Measured (us; tiles of 256 x 256, 256 x 128, 128 x 128,
-// 64 x 64):
-//   power-of-two scales      4096 x 4096 x 4096     56    71    80   133
-//                            3000 x 3000 x 3000     42    56    52    65
-//                            2048 x 4096 x 8192     81    63    73   125
-//                            2048 x 2048 x 2048     29    21    19    22
+// lowers the clock).  Fitted to 100 products of 20 shapes, of which the measured
+// best or one within 3% of it is taken.  Measured (us; tiles of 256 x 256, 256 x 128,
+// 128 x 128, 64 x 64):
+//   power-of-two scales      4096 x 4096 x 4096     56    71    80
+//                            3000 x 3000 x 3000     42    56    52    58
+//                            2048 x 4096 x 8192     81    63    73
+//                            2048 x 2048 x 2048     29    21    18    18
 //                            1000 x 1000 x 1000     22    16    11     7
-//   fp32 scales              4096 x 4096 x 4096     75          86   143
-//                            2048 x 4096 x 8192    124          87   136
-//   fp32 scales and results  4096 x 4096 x 4096                140   222
-//                            512 x 2048 x 2048                  25    15
-//   powers of two, fp32 res. 4096 x 4096 x 4096                127   211
+//   fp32 scales              4096 x 4096 x 4096     75          86
+//                            2048 x 4096 x 8192    124          87
+//                            2048 x 2048 x 2048     39          20    19
+//   fp32 scales and results  3000 x 3000 x 3000                 80    86
+//                            1537 x 1283 x 2051                 32    26
+//                            512 x 2048 x 2048                  25    14
+//   powers of two, fp32 res. 3000 x 3000 x 3000                 72    79
 // (fp32 results: the widened fragments leave no registers for tiles of 256 x 256,
 // which took 151 us with spilled ones.)  Tiles of 64 x 64 that leave CUs idle are
 // split along k, from 4 stages each: 300 x 300 x 8000 (25 tiles) 30 us in one piece,
@@ -90,10 +91,10 @@ struct TileCost {
 };
 constexpr TileCost kCosts[4][4] = {
     {{k256, 256, 256, 1, 13.0, 1.00, 1.33}, {k256x128, 256, 128, 1, 9.5, 0.69, 0.82},
-     {k128, 128, 128, 2, 6.5, 0.70, 1.03}, {k64, 64, 64, 2, 3.5, 0.37, 0.45}},
-    {{k256, 256, 256, 1, 11.0, 1.70, 2.00}, {}, {k128, 128, 128, 2, 6.5, 0.84, 1.24}, {k64, 64, 64, 2, 3.7, 0.42, 0.51}},
-    {{}, {}, {k128, 128, 128, 2, 8.0, 1.22, 1.98}, {k64, 64, 64, 2, 4.2, 0.66, 0.82}},
-    {{}, {}, {k128, 128, 128, 2, 7.5, 1.15, 1.80}, {k64, 64, 64, 2, 4.0, 0.60, 0.79}}};
+     {k128, 128, 128, 2, 6.5, 0.70, 1.03}, {k64, 64, 64, 4, 3.5, 0.40, 0.88}},
+    {{k256, 256, 256, 1, 11.0, 1.70, 2.00}, {}, {k128, 128, 128, 2, 6.5, 0.84, 1.24}, {k64, 64, 64, 4, 3.5, 0.45, 0.98}},
+    {{}, {}, {k128, 128, 128, 2, 8.0, 1.22, 1.98}, {k64, 64, 64, 4, 4.0, 0.60, 1.55}},
+    {{}, {}, {k128, 128, 128, 2, 7.5, 1.15, 1.80}, {k64, 64, 64, 4, 4.1, 0.55, 1.42}}};
 
 Plan plan_fp8(int m, int n, int k, Sum sum) {
     const int kblocks = (int)ceil_div(k, kBlockK);
@@ -115,7 +116,8 @@ Plan plan_fp8(int m, int n, int k, Sum sum) {
             const int64_t round = (int64_t)kCus * s.resident, rest = groups % round;
             double t = (double)(groups / round) * (s.fixed + p.per * s.full);
             if (rest > 0) {
-                const double fill = s.resident == 1 ? (double)rest / kCus : rest > kCus ? 1.0 : 0.0;
+                const double fill = s.resident == 1 ? (double)rest / kCus
+                                                    : (double)(ceil_div(rest, kCus) - 1) / (s.resident - 1);
                 t += s.fixed + p.per * (s.one + (s.full - s.one) * fill);
             }
             if (p.splits > 1) t += 3.0 + p.splits * (0.15 + 0.8e-6 * m * n);   // join_parts
