@@ -360,8 +360,8 @@ __global__ __launch_bounds__(256, 1) void product_pipe(ProductArgs g) {
 // stages on their way.  Rows of a wave are 16 i + q (block i, q = lane % 16),
 // columns 4 q + j: a lane holds 4 neighbouring columns (its blocks j) of 4
 // neighbouring rows (an accumulator), so it writes 8 bytes in either direction.
-template <bool SPLIT, Product KIND, int WR, int WC, int M, int S>
-__global__ __launch_bounds__(64 * WR * WC, 2) void product_tile(ProductArgs g) {
+template <bool SPLIT, Product KIND, int WR, int WC, int M, int S, int OCC>
+__global__ __launch_bounds__(64 * WR * WC, OCC) void product_tile(ProductArgs g) {
     constexpr int kWaves = WR * WC, kTm = WR * M * 16, kTn = WC * 64, kBuf = (kTm + kTn) * kStageRowBytes;
     constexpr int kCopyA = kTm / 8 / kWaves, kCopyB = kTn / 8 / kWaves;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S * kBuf];
@@ -490,6 +490,7 @@ struct Buffers {
 // How a product of rows x cols (padded) and `stages` stages is launched.
 struct ProductPlan {
     int tm, tn;                   // tiles: 256 x 256, 256 x 128 (the pipeline), 128 x 128, 64 x 64
+    int resident;                 // workgroups a CU holds (64 x 64: 2 with four stage buffers, 4 with two)
     int mt, nt, tiles;            // per matrix
     int64_t whole, rest;          // tiles with one workgroup, and split ones
     int splits, per;
@@ -499,22 +500,25 @@ struct ProductPlan {
 // has `fixed`, then per stage `one` while a CU has one workgroup and `full` with all of
 // `resident` (of one resident: while few CUs work, and when all do); then the
 // writing, or the sums' way through memory and their joining.  Fitted to the best of
-// 10 to 60 launches each of 54 products (64 x 64 tiles a, 128 x 128 b, 256 x 128 c, 256 x
-// 256 d; /n: split in n, +/n: the last round's); what it takes is 0.4% slower than the
-// best on average, 8% at most.  Measured (us):
+// 10 to 60 launches each of 54 products (64 x 64 tiles a, with two stage buffers and
+// four workgroups a CU a', 128 x 128 b, 256 x 128 c, 256 x 256 d; /n: split in n, +/n:
+// the last round's); what it takes is 0.5% slower than the best on average, 12% at
+// most.  Measured (us):
 //   r = c = 4096, one part, A    d 93, b 100, b/2 102, b+/8 77, b+/2 87
 //                           X    d 108, b 123, c 126
-//   r = c = 2048, one part, A    b 25, a 27, b/2 24, a+/8 24;  two parts: b/3 45, c/6 54
+//   r = c = 2048, one part, A    a' 20, b 25, a 27, b/2 24, a+/8 24;  two parts: b/3 45, d/6 54
+//   8 of 768 x 768, one part, A  a' 11, a 13, b 13
+//   r = c = 1024, one part, A    a 9, a' 12
 //   1024 x 8192, two parts, A    b/12 47, b/8 56, d/12 65;  X: c 62, b 64, d 93
-//   r = c = 1024, two parts, A   a/3 18, b/4 18, a 29
+//   r = c = 1024, two parts, A   a/3 18, a'/6 16, b/4 18, a 29
 //   320 x 896, two parts, A      a/4 11, a 22, b/4 16
 ProductPlan plan_product(int batch, int rows, int cols, int stages, bool sym) {
     struct Size {
         int tm, tn, resident;
         double fixed, one, full;
     };
-    constexpr Size sizes[] = {{64, 64, 2, 2.5, 0.42, 0.44}, {128, 128, 2, 3.9, 0.74, 0.90}, {256, 128, 1, 4.6, 0.89, 0.89},
-                              {256, 256, 1, 8.1, 1.21, 1.65}};
+    constexpr Size sizes[] = {{64, 64, 2, 3.7, 0.40, 0.48}, {64, 64, 4, 3.4, 0.48, 0.78}, {128, 128, 2, 4.1, 0.74, 0.95},
+                              {256, 128, 1, 4.9, 0.93, 0.93}, {256, 256, 1, 10.2, 1.22, 1.65}};
     const double entries = (double)batch * rows * cols * (sym ? 0.5 : 1.0);
     ProductPlan best = {};
     double least = 0.0;
@@ -523,13 +527,15 @@ ProductPlan plan_product(int batch, int rows, int cols, int stages, bool sym) {
         ProductPlan p;
         p.tm = s.tm;
         p.tn = s.tn;
+        p.resident = s.resident;
         p.mt = (int)ceil_div(rows, s.tm);
         p.nt = (int)ceil_div(cols, s.tn);
         p.tiles = sym ? p.mt * (p.mt + 1) / 2 : p.mt * p.nt;
         const int64_t all = (int64_t)p.tiles * batch, round = (int64_t)kCus * s.resident;
         auto rounds = [&](int64_t groups) {
             const int64_t left = groups % round;
-            const double fill = s.resident == 1 ? (double)left / kCus : left > kCus ? 1.0 : 0.0;
+            const double fill = s.resident == 1 ? (double)left / kCus
+                                                : (double)(ceil_div(left, kCus) - 1) / (s.resident - 1);
             return (double)(groups / round) * s.full + (left ? s.one + (s.full - s.one) * fill : 0.0);
         };
         for (int want = 1; want <= 16; ++want)
@@ -539,8 +545,8 @@ ProductPlan plan_product(int batch, int rows, int cols, int stages, bool sym) {
                 p.per = (int)ceil_div(stages, want);
                 p.splits = (int)ceil_div(stages, p.per);
                 if (want > 1 && (p.per < 4 || p.rest == 0)) continue;
-                double t = s.fixed + stages * rounds(p.whole) + p.per * rounds(p.rest * p.splits) + entries * 0.7e-6;
-                if (p.rest > 0) t += 4.8 + 0.26 * p.splits + p.rest * s.tm * s.tn * (0.25e-6 + 1.0e-6 * p.splits) + (some ? 0.5 * s.fixed : 0.0);
+                double t = s.fixed + stages * rounds(p.whole) + p.per * rounds(p.rest * p.splits) + entries * 0.5e-6;
+                if (p.rest > 0) t += 4.2 + p.splits * (0.22 + 1.1e-6 * p.rest * s.tm * s.tn) + (some ? 0.2 * s.fixed : 0.0);
                 if (least == 0.0 || t < least) {
                     least = t;
                     best = p;
@@ -607,8 +613,9 @@ void launch_product(ProductArgs &g, const ProductPlan &p, int batch, hipStream_t
     g.whole_chunk = (int)ceil_div(p.whole, kXcds);
     g.rest_chunk = (int)ceil_div(p.rest * p.splits, kXcds);
     const unsigned grid = (unsigned)(kXcds * (g.whole_chunk + g.rest_chunk));
-    if (p.tm == 64) product_tile<SPLIT, KIND, 4, 1, 1, 4><<<grid, 256, 0, st>>>(g);
-    else if (p.tm == 128) product_tile<SPLIT, KIND, 2, 2, 4, 2><<<grid, 256, 0, st>>>(g);
+    if (p.resident == 4) product_tile<SPLIT, KIND, 4, 1, 1, 2, 4><<<grid, 256, 0, st>>>(g);
+    else if (p.tm == 64) product_tile<SPLIT, KIND, 4, 1, 1, 4, 2><<<grid, 256, 0, st>>>(g);
+    else if (p.tm == 128) product_tile<SPLIT, KIND, 2, 2, 4, 2, 2><<<grid, 256, 0, st>>>(g);
     else if (p.tn == 256) product_pipe<SPLIT, KIND, 8><<<grid, 256, 0, st>>>(g);
     else if constexpr (!symmetric(KIND)) product_pipe<SPLIT, KIND, 4><<<grid, 256, 0, st>>>(g);
     if (p.rest > 0) {
