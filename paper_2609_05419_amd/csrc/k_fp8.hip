@@ -78,7 +78,9 @@ constexpr int kFewRows = 32;
 // which took 151 us with spilled ones.)  Tiles of 64 x 64 that leave CUs idle are
 // split along k, from 4 stages each: 300 x 300 x 8000 (25 tiles) 30 us in one piece,
 // 11.5 in 8; 64 x 4096 x 4096 (64) 16, and 10.7 in 4; 1000 x 1000 x 1000 (256) 6.9, and
-// 12.1 in 2.
+// 12.1 in 2.  (Near the edge the launch of its own that the joining takes decides:
+// 333 x 1283 x 2051 with 126 tiles takes the GPU 12.1 us, in 2 splits 10.8, but a linear
+// layer of it, launch by launch, 16 and 18.)
 struct Plan {
     bool few;
     TileSize size;
