@@ -493,3 +493,52 @@ def test_graphs(o2m):
         torch.cuda.synchronize()
         for (_, _, _, out), want in zip(graphs, eager):
             assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]), seed
+
+
+# ---- beyond 2^31 entries, and the largest update ----------------------------------
+
+def same_bits(a, b):
+    return all(torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8)) for x, y in zip(a, b))
+
+
+def test_quantize_past_32_bits(o2m):
+    """Rows and columns at the end of a matrix of more than 2^31 entries."""
+    rows, k = 66000, 33000
+    x = torch.randn((rows, k), dtype=torch.bfloat16, device=DEV)
+    q, qt = o2m.quantize_fp8_pair(x)
+    assert same_bits((q.values[-200:], q.scales[-200:]), o2m.quantize_fp8(x[-200:]))
+    assert same_bits((qt.values[-200:], qt.scales[-200:]), o2m.quantize_fp8(x[:, -200:].t()))
+    only = o2m.quantize_fp8(x)
+    assert same_bits((only.values[-200:], only.scales[-200:]), (q.values[-200:], q.scales[-200:]))
+
+
+@pytest.mark.parametrize("scales,dtype", [("pow2", torch.bfloat16), ("float32", torch.float16), ("pow2", torch.float32)])
+def test_gemm_past_32_bits(o2m, scales, dtype):
+    """A result of more than 2^31 entries, in either order: its first and last rows."""
+    m, n, k = 66000, 33000, 40
+    A = o2m.quantize_fp8(matrix(m, k, 61, spread=0.5), scales=scales)
+    B = o2m.quantize_fp8(matrix(n, k, 62, spread=0.5), scales=scales)
+    a, b = R.values64(A, 1), R.values64(B, 1)
+    for out in (torch.empty((m, n), dtype=dtype, device=DEV), torch.empty((n, m), dtype=dtype, device=DEV).t()):
+        o2m.gemm_fp8(A, B, out=out)
+        for part in (slice(0, 30), slice(m - 30, m)):
+            R.check_product(out[part], a[part], b, dtype)
+
+
+def test_orthogonalize_largest(o2m):
+    """2^29 entries, one per row not zero: X stays such a matrix, of the scalars x <-
+    a x + b x^3 + c x^5.  All sums have one term, so what is off is the roundings of
+    held numbers, u = 2^-21 relative each (two fp16 parts): X before the first
+    step, with the norm's inverse below u / 4, and in a step B (A, of at most 0.02
+    in B, adds below 0.05 u) and X, with three fp32 roundings of u / 4: below 3 u a
+    step, 8 u in all with the last rounding."""
+    r, c = 16384, 32768
+    g = torch.zeros((r, c), device=DEV)
+    g.diagonal().fill_(3.0)
+    x = o2m.orthogonalize(g, steps=2)
+    s = 1.0 / 128
+    for _ in range(2):
+        s = R.COEF[0] * s + R.COEF[1] * s ** 3 + R.COEF[2] * s ** 5
+    assert (x.diagonal().double() - s).abs().max().item() <= 8 * 2.0 ** -21 * s
+    x.diagonal().zero_()
+    assert not x.any()
