@@ -25,7 +25,7 @@ from typing import NamedTuple
 
 import torch
 
-from . import _L, _check, _stream
+from . import O2MError, _L, _check, _stream
 
 __all__ = ["Fp8Operand", "quantize_fp8", "quantize_fp8_pair", "gemm_fp8", "linear_fp8", "linear_fp8_backward",
            "orthogonalize"]
@@ -58,6 +58,8 @@ _SCALES = {"pow2": 0, "float32": 1}
 _SCALE_DTYPES = {"pow2": torch.float8_e8m0fnu, "float32": torch.float32}
 _SCALE_KINDS = {torch.float8_e8m0fnu: 0, torch.uint8: 0, torch.float32: 1}
 BLOCK = 128
+_LARGEST = (1 << 31) - 1   # what the C calls' sizes hold: ctypes would drop the bits above
+_ERR_STEPS, _MOST_STEPS = -28, 64
 
 
 class Fp8Operand(NamedTuple):
@@ -73,6 +75,11 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 def _here(x: torch.Tensor, name: str) -> None:
     if not x.is_cuda or x.get_device() != _current_device():   # (get_device() is -1 on the CPU)
         raise ValueError(f"{name} must be a tensor on the current device")
+
+
+def _fits(shape, name: str) -> None:
+    if max(shape) > _LARGEST:
+        raise ValueError(f"{name}: sizes reach 2^31 - 1 at most, got {tuple(shape)}")
 
 
 def _type_of(x: torch.Tensor, name: str) -> int:
@@ -103,6 +110,7 @@ def _matrix(x: torch.Tensor, name: str):
     shape = x.shape
     if len(shape) != 2:
         raise ValueError(f"{name} must be a matrix, got {len(shape)} dimensions")
+    _fits(shape, name)
     _here(x, name)
     s0, s1 = x.stride()
     if s1 == 1 and shape[0] > 1 and shape[1] > 1:
@@ -119,6 +127,7 @@ def _operand(x, name: str) -> _Operand:
     shape, s_shape = q.shape, s.shape
     if len(shape) != 2 or len(s_shape) != 2:
         raise ValueError(f"{name}: values and scales must be matrices")
+    _fits(shape, name)
     _here(q, name)
     _here(s, name)
     kind = _SCALE_KINDS.get(s.dtype)
@@ -317,6 +326,9 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750
     t = _type_of(G, "G")
     if G.dim() not in (2, 3):
         raise ValueError(f"G must be a matrix or a batch of matrices, got {G.dim()} dimensions")
+    _fits(G.shape, "G")
+    if not 0 <= steps <= _MOST_STEPS:
+        raise O2MError(_ERR_STEPS, "orthogonalize")
     _here(G, "G")
     rows, cols = G.shape[-2:]
     batch = G.size(0) if G.dim() == 3 else 1
@@ -332,8 +344,8 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750
     oo, ldo = _order(rows, cols, out.stride(-2), out.stride(-1), "out")
     flat = [float(c) for k in coefficients for c in (k if hasattr(k, "__len__") else (k,))]
     if len(flat) == 3:
-        flat = flat * max(steps, 0)
-    if steps >= 0 and len(flat) != 3 * steps:
+        flat = flat * steps
+    if len(flat) != 3 * steps:
         raise ValueError(f"coefficients must be one triple or {steps} of them")
     coef = (ctypes.c_double * max(len(flat), 1))(*flat)
     ws, at, nbytes = _scratch(_L.o2m_orthogonalize_workspace(batch, rows, cols, t), out, stream)
