@@ -310,6 +310,20 @@ def linear_fp8_backward(dY: torch.Tensor, Xt, Wt, dtype=torch.float8_e4m3fn, dW:
     of the transposes, k rows of tokens and k rows of n values, as
     quantize_fp8_pair makes them in the forward pass; dY (tokens x n) is
     quantized to ``dtype`` in blocks of 1 x 128 along both its axes."""
+    if dY.dim() != 2:
+        raise ValueError(f"dY must be a matrix, got {dY.dim()} dimensions")
+    (tokens, n), k = dY.shape, Wt[0].size(0)
+    # both products are checked here, so that none is computed when the other cannot be
+    if tuple(Xt[0].shape) != (k, tokens) or tuple(Wt[0].shape) != (k, n):
+        raise ValueError(f"Xt and Wt must have k rows both, of tokens = {tokens} and n = {n} values, got "
+                         f"{tuple(Xt[0].shape)} and {tuple(Wt[0].shape)}")
+    if _SCALE_KINDS.get(Xt[1].dtype) != _SCALE_KINDS.get(Wt[1].dtype):
+        raise TypeError("Xt and Wt must have the same kind of scales")
+    if dW is None:
+        if accumulate:
+            raise ValueError("accumulate needs dW")
+    elif tuple(dW.shape) != (n, k):
+        raise ValueError(f"dW must be of shape {(n, k)}, got {tuple(dW.shape)}")
     scales = "float32" if Wt[1].dtype == torch.float32 else "pow2"
     dy, dyt = quantize_fp8_pair(dY, (1, BLOCK), dtype, scales, stream=stream)
     dX = gemm_fp8(dy, Wt, dtype=dY.dtype, stream=stream)

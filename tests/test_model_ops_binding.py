@@ -20,13 +20,13 @@ def wide(rows, cols, dtype=torch.bfloat16):
 @pytest.mark.parametrize("n", FAR)
 def test_sizes_past_32_bits(n):
     fp8 = torch.float8_e4m3fn
-    q = (wide(3, 16, fp8), wide(3, 1, torch.float32))
     long_k, many = (wide(3, n, fp8), wide(3, -(-n // 128), torch.float32)), (wide(n, 16, fp8), wide(n, 1, torch.float32))
     calls = [lambda: o2m.quantize_fp8(wide(1, n)), lambda: o2m.quantize_fp8(wide(n, 1)),
              lambda: o2m.quantize_fp8(wide(n, 1), out=many), lambda: o2m.quantize_fp8_pair(wide(n, 2)),
-             lambda: o2m.gemm_fp8(many, q), lambda: o2m.gemm_fp8(long_k, q), lambda: o2m.linear_fp8(wide(2, 16), many),
+             lambda: o2m.gemm_fp8(many, many), lambda: o2m.gemm_fp8(long_k, long_k), lambda: o2m.linear_fp8(wide(2, 16), many),
              lambda: M._operand(long_k, "W"), lambda: M._matrix(wide(n, 16), "X"),   # (whichever comes first)
-             lambda: o2m.linear_fp8_backward(wide(n, 3), q, q),
+             lambda: o2m.linear_fp8_backward(wide(n, 3), (wide(2, n, fp8), wide(2, -(-n // 128), torch.float32)),
+                                             (wide(2, 3, fp8), wide(2, 1, torch.float32))),
              lambda: o2m.orthogonalize(wide(n, 1)), lambda: o2m.orthogonalize(wide(1, n)),
              lambda: o2m.orthogonalize(torch.zeros(1).expand(n, 2, 2))]
     for call in calls:
@@ -39,3 +39,26 @@ def test_steps_past_32_bits():
         with pytest.raises(o2m.O2MError, match="steps") as e:
             o2m.orthogonalize(torch.zeros((3, 4)), steps=steps)
         assert e.value.status == -28
+
+
+# ---- operands of a backward step that do not belong together ---------------------
+
+def test_backward_of_operands_of_different_layers():
+    """Xt and Wt of different k, of other tokens or outputs than dY, or of two kinds of scales: refused
+    before dY is quantized."""
+    def op(rows, k, s=torch.float32):
+        return torch.zeros((rows, k), dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros((rows, -(-k // 128)), dtype=s)
+    dy = torch.zeros((32, 48))   # 32 tokens, n = 48
+    for xt, wt, what in ((op(64, 32), op(80, 48), "k rows"), (op(64, 16), op(64, 48), "tokens"),
+                         (op(64, 32), op(64, 32), "n = 48"), (op(64, 32, torch.uint8), op(64, 48), "kind of scales"),
+                         (op(64, 32), op(64, 48, torch.uint8), "kind of scales")):
+        error = TypeError if "scales" in what else ValueError
+        with pytest.raises(error, match=what):
+            o2m.linear_fp8_backward(dy, xt, wt)
+    with pytest.raises(ValueError, match="matrix"):
+        o2m.linear_fp8_backward(torch.zeros(48), op(64, 32), op(64, 48))
+    for dw in (torch.zeros((48, 65)), torch.zeros((64, 48)), torch.zeros(48)):
+        with pytest.raises(ValueError, match="dW"):
+            o2m.linear_fp8_backward(dy, op(64, 32), op(64, 48), dW=dw)
+    with pytest.raises(ValueError, match="dW"):
+        o2m.linear_fp8_backward(dy, op(64, 32), op(64, 48), accumulate=True)
