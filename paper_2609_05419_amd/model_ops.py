@@ -13,10 +13,12 @@ An 8-bit operand is a pair ``(values, scales)``: ``values`` of shape (rows, k)
 in ``torch.float8_e4m3fn`` or ``torch.float8_e5m2``, k running contiguously and
 rows starting at multiples of 16 bytes, ``scales`` of shape (rows, ceil(k /
 128)) for blocks of 1 x 128 or (ceil(rows / 128), ceil(k / 128)) for blocks of
-128 x 128, in ``torch.float8_e8m0fnu`` (powers of two) or ``torch.float32``.  The
-matrix it stands for is each value times its block's scale.  ``quantize_fp8``
-makes one.  Other matrices may be row-major or column-major.  There is no
-autograd here: the backward products are calls of their own.
+128 x 128, in ``torch.float8_e8m0fnu`` (powers of two; or its bytes, in
+``torch.uint8``, which are what a torch without that type gets) or
+``torch.float32``.  The matrix it stands for is each value times its block's
+scale.  ``quantize_fp8`` makes one.  Other matrices may be row-major or
+column-major.  There is no autograd here: the backward products are calls of
+their own.
 """
 from __future__ import annotations
 
@@ -53,10 +55,13 @@ for _f in ("o2m_gemm_fp8_workspace", "o2m_linear_fp8_workspace", "o2m_orthogonal
     getattr(_L, _f).restype = _Z
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-_FORMATS = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+# (older releases of torch lack these types, and the package's other calls need none:
+# a type that is missing is only missed where it is asked for)
+_E4M3, _E5M2, _E8M0 = (getattr(torch, t, None) for t in ("float8_e4m3fn", "float8_e5m2", "float8_e8m0fnu"))
+_FORMATS = {t: i for i, t in enumerate((_E4M3, _E5M2)) if t is not None}
 _SCALES = {"pow2": 0, "float32": 1}
-_SCALE_DTYPES = {"pow2": torch.float8_e8m0fnu, "float32": torch.float32}
-_SCALE_KINDS = {torch.float8_e8m0fnu: 0, torch.uint8: 0, torch.float32: 1}
+_SCALE_DTYPES = {"pow2": _E8M0 or torch.uint8, "float32": torch.float32}
+_SCALE_KINDS = {_SCALE_DTYPES["pow2"]: 0, torch.uint8: 0, torch.float32: 1}
 BLOCK = 128
 _LARGEST = (1 << 31) - 1   # what the C calls' sizes hold: ctypes would drop the bits above
 _ERR_STEPS, _MOST_STEPS = -28, 64
@@ -202,7 +207,7 @@ def _written(out, shape, what):
     return _operand(out, what)
 
 
-def quantize_fp8(X: torch.Tensor, block=(1, 128), dtype=torch.float8_e4m3fn, scales: str = "pow2", out=None,
+def quantize_fp8(X: torch.Tensor, block=(1, 128), dtype=_E4M3, scales: str = "pow2", out=None,
                  stream=None) -> Fp8Operand:
     """X (rows x k, float32, float16 or bfloat16) as an 8-bit operand: blocks of
     1 x 128 or 128 x 128, the last ones shorter.
@@ -225,7 +230,7 @@ def quantize_fp8(X: torch.Tensor, block=(1, 128), dtype=torch.float8_e4m3fn, sca
     return out
 
 
-def quantize_fp8_pair(X: torch.Tensor, block=(1, 128), dtype=torch.float8_e4m3fn, scales: str = "pow2", out=None,
+def quantize_fp8_pair(X: torch.Tensor, block=(1, 128), dtype=_E4M3, scales: str = "pow2", out=None,
                       stream=None) -> tuple[Fp8Operand, Fp8Operand]:
     """The operands of X and of its transpose from one reading of X (what a
     layer's forward product and its backward products take of X, W or dY).
@@ -303,7 +308,7 @@ def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None)
     return out
 
 
-def linear_fp8_backward(dY: torch.Tensor, Xt, Wt, dtype=torch.float8_e4m3fn, dW: torch.Tensor | None = None,
+def linear_fp8_backward(dY: torch.Tensor, Xt, Wt, dtype=_E4M3, dW: torch.Tensor | None = None,
                         accumulate: bool = False, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
     """(dX, dW) of Y = X W^T: dX = dY W (of dY's type) and dW = dY^T X (float32; into
     ``dW`` if given, added to it with ``accumulate``).  Xt and Wt are the operands

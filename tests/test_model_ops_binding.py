@@ -1,10 +1,16 @@
 """What the binding of the products of trained models checks before it allocates
 or calls anything (no GPU, and no memory behind the large shapes)."""
+import os
+import subprocess
+import sys
+
 import pytest
 
 torch = pytest.importorskip("torch")
 import paper_2609_05419_amd as o2m  # noqa: E402
 from paper_2609_05419_amd import model_ops as M  # noqa: E402
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 # ---- sizes past 32 bits ----------------------------------------------------------
@@ -62,3 +68,28 @@ def test_backward_of_operands_of_different_layers():
             o2m.linear_fp8_backward(dy, op(64, 32), op(64, 48), dW=dw)
     with pytest.raises(ValueError, match="dW"):
         o2m.linear_fp8_backward(dy, op(64, 32), op(64, 48), accumulate=True)
+
+
+# ---- a torch without the 8-bit types ---------------------------------------------
+
+@pytest.mark.parametrize("lacks", [["float8_e8m0fnu"], ["float8_e8m0fnu", "float8_e4m3fn", "float8_e5m2"]])
+def test_import_without_8_bit_types(lacks):
+    """The package, the 2M calls with it, needs none of torch's 8-bit types: without them
+    scales of powers of two are bytes, and a call that takes 8-bit values says what it lacks."""
+    code = f"""
+import torch
+for name in {lacks!r}:
+    delattr(torch, name)
+import paper_2609_05419_amd as o2m
+from paper_2609_05419_amd import model_ops as M
+o2m.moduli(3)
+assert M._SCALE_DTYPES["pow2"] == torch.uint8 and M._SCALE_KINDS[torch.uint8] == 0
+x = torch.zeros((2, 16))
+try:
+    o2m.quantize_fp8(x)
+except (ValueError if hasattr(torch, "float8_e4m3fn") else TypeError) as e:
+    print(e)
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    assert ("float8_e4m3fn" if len(lacks) == 3 else "current device") in r.stdout
