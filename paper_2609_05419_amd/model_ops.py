@@ -18,7 +18,8 @@ rows starting at multiples of 16 bytes, ``scales`` of shape (rows, ceil(k /
 ``torch.float32``.  The matrix it stands for is each value times its block's
 scale.  ``quantize_fp8`` makes one.  Other matrices may be row-major or
 column-major.  There is no autograd here: the backward products are calls of
-their own.
+their own, and an input that requires a gradient is refused while gradients are
+recorded (``torch.no_grad()`` or ``detach()`` says that none is wanted).
 """
 from __future__ import annotations
 
@@ -88,6 +89,10 @@ def _fits(shape, name: str) -> None:
 
 
 def _type_of(x: torch.Tensor, name: str) -> int:
+    """The C code of an input's type; of one whose gradient nobody would get, an error."""
+    if x.requires_grad and torch.is_grad_enabled():
+        raise RuntimeError(f"{name} requires a gradient, which this call does not pass on: call it under torch.no_grad() "
+                           f"or on {name}.detach(), and take the gradients from linear_fp8_backward")
     t = _TYPES.get(x.dtype)
     if t is None:
         raise TypeError(f"{name} must be float32, float16 or bfloat16, got {x.dtype}")

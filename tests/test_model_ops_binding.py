@@ -93,3 +93,23 @@ except (ValueError if hasattr(torch, "float8_e4m3fn") else TypeError) as e:
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     assert ("float8_e4m3fn" if len(lacks) == 3 else "current device") in r.stdout
+
+
+# ---- tensors that require a gradient ---------------------------------------------
+
+def test_gradients_are_not_lost_silently():
+    """The results carry no graph, so an input that requires a gradient is refused while
+    gradients are recorded; without recording, or detached, it passes (to the next check)."""
+    def op(rows, k):
+        return torch.zeros((rows, k), dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros((rows, -(-k // 128)))
+    x = torch.zeros((4, 32), requires_grad=True)
+    w, xt, wt = op(48, 32), op(16, 4), op(16, 32)
+    calls = [lambda x: o2m.quantize_fp8(x), lambda x: o2m.quantize_fp8_pair(x), lambda x: o2m.linear_fp8(x, w),
+             lambda x: o2m.linear_fp8_backward(x, xt, wt), lambda x: o2m.orthogonalize(x),
+             lambda x: o2m.quantize_fp8(2 * x)]
+    for call in calls:
+        with pytest.raises(RuntimeError, match="gradient"):
+            call(x)
+        for y in (x.detach(), x):
+            with torch.set_grad_enabled(y is not x), pytest.raises(ValueError, match="current device"):
+                call(y)
