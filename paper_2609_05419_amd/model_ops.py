@@ -289,8 +289,8 @@ def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None)
     """The linear layer Y = X W^T: X (tokens x k, row-major) is quantized to e4m3
     in blocks of 1 x 128 with W's kind of scales and multiplied with the operand
     W (n rows of k); Y (tokens x n, row-major) has X's type."""
-    w = _operand(W, "W")
     t = _type_of(X, "X")
+    w = _operand(W, "W")
     order, ldx = _matrix(X, "X")
     tokens, k = X.shape
     n = W[0].size(0)
