@@ -147,6 +147,15 @@ __global__ __launch_bounds__(kThreads) void ortho_small(SmallArgs g, SmallCoef c
         hold4<SPLIT>(lines, p, q + 4, v4f{y[4], y[5], y[6], y[7]});
     }
     __syncthreads();
+    if (g.steps == 0) {   // X itself
+        for (int i = tid; i < g.r * g.c; i += kThreads) {
+            const int row = i / g.c, col = i - row * g.c;
+            const f16 *v = x.hi + row * x.pitch + col;
+            store_any(g.O, b * g.o_batch + row * g.o_row + col * g.o_col, g.g.type,
+                      ((float)v[0] + (SPLIT ? (float)v[x.lo] : 0.0f)) * (1.0f / (1 << kScaleX)));
+        }
+        return;   // whole workgroup
+    }
 
     const int rt = g.rp / 32, ct = g.cp / 32;
     const int quad = lane >> 4, q = lane & 15;
@@ -221,9 +230,9 @@ int64_t lds_bytes(int r, int c, bool split) {
 }  // namespace
 
 // Matrices that fit, whose products are one round of the waves.
-bool ortho_is_small(int r, int c, bool split, int steps) {
+bool ortho_is_small(int r, int c, bool split) {
     const int64_t rt = ceil_div(r, 32), ct = ceil_div(c, 32);
-    return steps > 0 && rt * ct <= kWaves && lds_bytes(r, c, split) <= kLdsBytes;
+    return rt * ct <= kWaves && lds_bytes(r, c, split) <= kLdsBytes;
 }
 
 hipError_t launch_ortho_small(const OrthoArgs &o, bool split, hipStream_t st) {

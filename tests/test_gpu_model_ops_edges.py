@@ -1,0 +1,45 @@
+"""The products of trained models at their edges: calls at the limits of a kernel's
+range, results and inputs in one memory, and steps of the update one by one."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+import model_reference as R  # noqa: E402
+from test_gpu_model_ops import DEV, E4M3, TYPES, matrix, o2m, padded_operand  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- the update of small matrices: one workgroup each ------------------------------
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 200), (96, 80), (33, 90), (64, 64), (150, 60)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_small_update_without_steps(o2m, rows, cols, dtype):  # noqa: F811
+    """X = G / (||G|| + eps), held in one or two fp16 parts of X 2^14 and rounded to the type: half a
+    step of each of the two roundings, and one of 2^-23 for the quotient in fp32; the numbers that fp16
+    holds end at 2^-24, so an entry may be off by half of that, 2^-39 of X."""
+    for order in ("row", "col"):
+        g = matrix(rows, cols, 13, torch.float32, order, spread=1.0)
+        g = g.to(dtype) if order == "row" else g.t().contiguous().to(dtype).t()
+        print("no steps", rows, cols, dtype, order, flush=True)
+        got = o2m.orthogonalize(g, steps=0).double().cpu().numpy()
+        exact = g.double().cpu().numpy()
+        exact = exact / (np.linalg.norm(exact) + 1e-7)
+        one = R.half_step(torch.float16)
+        u = (one if dtype == torch.bfloat16 else 2 * one * one) + R.half_step(dtype) + 2.0 ** -23
+        tiny = {torch.float32: 0.0, torch.float16: 2.0 ** -25, torch.bfloat16: 0.0}[dtype] + 2.0 ** -39
+        assert (np.abs(got - exact) <= 1.01 * u * np.abs(exact) + tiny).all()
+
+
+@pytest.mark.parametrize("steps", [0, 2])
+def test_most_small_updates(o2m, steps):  # noqa: F811
+    """65535 matrices in one call, each as if it were alone, and next to no scratch memory."""
+    g = torch.randn((65535, 20, 33), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    x = o2m.orthogonalize(g, steps=steps)
+    torch.cuda.synchronize()
+    assert torch.cuda.max_memory_allocated() - before <= x.numel() * 4 + (4 << 20)
+    for i in (0, 1, 40000, 65534):
+        assert torch.equal(x[i], o2m.orthogonalize(g[i], steps=steps))

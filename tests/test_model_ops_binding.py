@@ -113,3 +113,17 @@ def test_gradients_are_not_lost_silently():
         for y in (x.detach(), x):
             with torch.set_grad_enabled(y is not x), pytest.raises(ValueError, match="current device"):
                 call(y)
+
+
+# ---- scratch memory ---------------------------------------------------------------
+
+def test_scratch_of_small_updates():
+    """Matrices that one workgroup keeps in LDS need none, however many (21 GB were asked for
+    65535 of 96 x 80); others theirs."""
+    need = o2m._L.o2m_orthogonalize_workspace
+    for t in range(3):
+        for rows, cols in ((1, 1), (96, 80), (80, 96), (128, 128), (64, 256), (33, 90)):
+            small = (rows, cols) not in ((128, 128), (64, 256)) or t == 2   # (fp32 and fp16 are held twice as long)
+            for batch in (1, 65535):
+                assert (need(batch, rows, cols, t) <= 256) == small, (t, rows, cols, batch)
+        assert need(2, 300, 200, t) > 2 * 2 * 5 * 200 * 200
