@@ -152,6 +152,8 @@ o2m_status o2m_linear_fp8(int tokens, int n, int k, const void *X, int x_type, i
     const o2m_status s = check_workspace(o2m_linear_fp8_workspace(tokens, n, k), workspace, workspace_bytes);
     if (s != O2M_OK) return s;
     if (linear_is_fused(tokens, k)) return hip_fail(launch_linear_fused(tokens, n, k, X, x_type, ldx, *W, Y, ldy, st));
+    // (the product is checked before the tokens are quantized)
+    if (!gemm_fp8_fits(tokens, n, k, W->scale_type, x_type)) return O2M_ERR_SIZE;
     const o2m_fp8_operand q = kept_x(tokens, k, W->scale_type, workspace);
     const hipError_t e = launch_quantize(tokens, k, X, x_type, ldx, &q, nullptr, st);
     if (e != hipSuccess) return hip_fail(e);

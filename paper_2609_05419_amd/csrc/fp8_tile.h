@@ -231,7 +231,7 @@ hipError_t launch_tile(Fp8Args &g, hipStream_t st) {
     g.mt = (int)ceil_div(g.a.rows, T::kTm);
     g.nt = (int)ceil_div(g.b.rows, T::kTn);
     const int64_t chunk = ceil_div((int64_t)g.mt * g.nt, kXcds), grid = kXcds * chunk * g.splits;
-    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (!launch_fits(grid, T::kThreads)) return hipErrorInvalidValue;
     g.chunk = (int)chunk;
     fp8_tile<SUM, FA, FB, WB, WR, WC, M, OCC><<<(unsigned)grid, T::kThreads, 0, st>>>(g);
     return hipGetLastError();

@@ -152,10 +152,24 @@ size_t gemm_fp8_workspace(int m, int n, int k) {
     return sizeof(float) * (size_t)splits * (size_t)std::max(m * round_up64(n, 4), n * round_up64(m, 4));
 }
 
+static Sum sum_of(int scale_type, int type) {
+    const bool wide = type == O2M_TYPE_F32;
+    return scale_type == O2M_SCALES_POW2 ? (wide ? kWideScaled : kScaled) : wide ? kWide : kPartial;
+}
+
+bool gemm_fp8_fits(int m, int n, int k, int scale_type, int type) {
+    const Sum sum = sum_of(scale_type, type);
+    const Plan p = plan_fp8(m, n, k, sum);
+    if (p.few) return launch_fits(ceil_div(std::max(m, n), 16), 256);
+    const TileCost &s = kCosts[sum][p.size];
+    return launch_fits(round_up64(ceil_div(m, s.rows) * ceil_div(n, s.cols), kXcds) * p.splits,
+                       sum == kPartial && p.size == k256 ? 512 : 256);
+}
+
 hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const o2m_fp8_operand &B, void *C, int type,
                            int64_t ldc, bool accumulate, void *ws, hipStream_t st) {
     const bool wide = type == O2M_TYPE_F32;
-    const Plan p = plan_fp8(m, n, k, A.scale_type == O2M_SCALES_POW2 ? (wide ? kWideScaled : kScaled) : wide ? kWide : kPartial);
+    const Plan p = plan_fp8(m, n, k, sum_of(A.scale_type, type));
     if (p.few)
         return n <= m ? launch_few(n, m, k, B, A, C, type, 1, ldc, accumulate, st)
                       : launch_few(m, n, k, A, B, C, type, ldc, 1, accumulate, st);

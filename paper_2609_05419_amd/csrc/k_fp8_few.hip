@@ -195,6 +195,9 @@ void launch_waves(const FewArgs &g, hipStream_t st) {
     else if constexpr (!FUSED) few_rows<16, T, F, FUSED><<<grid, 1024, 0, st>>>(g);
 }
 
+// (256 threads where there are many workgroups)
+bool few_fits(int n) { return launch_fits(ceil_div(n, 16), 256); }
+
 template <int F>
 void launch_tokens(const FewArgs &g, hipStream_t st) {
     if (g.x.rows <= 16) launch_waves<1, F, false>(g, st);
@@ -208,6 +211,7 @@ bool linear_is_fused(int tokens, int k) { return tokens <= 16 && tokens * round_
 
 hipError_t launch_linear_fused(int tokens, int n, int k, const void *X, int x_type, int64_t ldx, const o2m_fp8_operand &W,
                                void *Y, int64_t ldy, hipStream_t st) {
+    if (!few_fits(n)) return hipErrorInvalidValue;
     FewArgs g = {};
     g.w = side_of(W, n);
     g.x.rows = tokens;
@@ -228,6 +232,7 @@ hipError_t launch_linear_fused(int tokens, int n, int k, const void *X, int x_ty
 // W: the operand with the many rows; entry (t, r) of Y at t y_tok + r y_row.
 hipError_t launch_few(int tokens, int n, int k, const o2m_fp8_operand &X, const o2m_fp8_operand &W, void *Y, int type,
                       int64_t y_tok, int64_t y_row, bool accumulate, hipStream_t st) {
+    if (!few_fits(n)) return hipErrorInvalidValue;
     FewArgs g = {};
     g.w = side_of(W, n);
     g.x = side_of(X, tokens);

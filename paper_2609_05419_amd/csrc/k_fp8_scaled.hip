@@ -131,7 +131,7 @@ hipError_t launch_pipe(Fp8Args &g, hipStream_t st) {
     g.mt = (int)ceil_div(g.a.rows, kPipeTile);
     g.nt = (int)ceil_div(g.b.rows, PipeShape<N>::kTn);
     const int64_t chunk = ceil_div((int64_t)g.mt * g.nt, kXcds);
-    if (kXcds * chunk > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (!launch_fits(kXcds * chunk, 256)) return hipErrorInvalidValue;
     g.chunk = (int)chunk;
     const unsigned grid = (unsigned)(kXcds * chunk);
     if (g.a.by_row && g.b.by_row) fp8_pipe<FA, FB, false, false, N><<<grid, 256, 0, st>>>(g);

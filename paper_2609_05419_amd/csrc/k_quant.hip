@@ -229,13 +229,14 @@ Dest dest_of(const o2m_fp8_operand *o) {
 template <class T>
 hipError_t launch(const QuantArgs &g, int64_t tiles, hipStream_t st) {
     if (g.across.values || g.along.block != 1) {
+        if (!launch_fits(tiles, kTileThreads)) return hipErrorInvalidValue;
         if (!g.across.values) quantize_tile<T, true, false><<<(unsigned)tiles, kTileThreads, 0, st>>>(g);
         else if (!g.along.values) quantize_tile<T, false, true><<<(unsigned)tiles, kTileThreads, 0, st>>>(g);
         else quantize_tile<T, true, true><<<(unsigned)tiles, kTileThreads, 0, st>>>(g);
         return hipGetLastError();
     }
     const int64_t by4 = ceil_div(g.lines * ceil_div(g.tiles_q, 4), 16), by1 = ceil_div((int64_t)g.lines * g.tiles_q, 16);
-    if (by1 > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (!launch_fits(by4 >= 2048 ? by4 : by1, 256)) return hipErrorInvalidValue;
     if (by4 >= 2048) quantize_rows<T, 4><<<(unsigned)by4, 256, 0, st>>>(g);
     else quantize_rows<T, 1><<<(unsigned)by1, 256, 0, st>>>(g);
     return hipGetLastError();
@@ -247,7 +248,6 @@ hipError_t launch_quantize(int lines, int len, const void *X, int type, int64_t 
                            const o2m_fp8_operand *across, hipStream_t st) {
     const int64_t tiles_q = ceil_div(len, 128), tiles = tiles_q * ceil_div(lines, 128);
     if (tiles <= 0) return hipSuccess;
-    if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
     const QuantArgs g = {X, ld, lines, len, (int)tiles_q, dest_of(along), dest_of(across)};
     switch (type) {
     case O2M_TYPE_F32: return launch<float>(g, tiles, st);

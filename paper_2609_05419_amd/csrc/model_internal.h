@@ -17,6 +17,9 @@ constexpr int kBlockK = 128;   // entries of a block along the inner dimension
 inline int64_t ceil_div(int64_t x, int64_t q) { return (x + q - 1) / q; }
 inline int64_t round_up64(int64_t x, int64_t q) { return ceil_div(x, q) * q; }
 
+// The runtime counts a launch's threads in 32 bits.
+inline bool launch_fits(int64_t groups, int threads) { return groups * threads <= 0xFFFFFFFFLL; }
+
 // Quantize the matrix of `lines` x `len` entries, entry (p, q) at X[p ld + q]:
 // along its lines into `along` and across them into `across` (rows of an
 // operand are lines, or entry positions q); either may be null.
@@ -27,6 +30,8 @@ hipError_t launch_quantize(int lines, int len, const void *X, int type, int64_t 
 hipError_t launch_gemm_fp8(int m, int n, int k, const o2m_fp8_operand &A, const o2m_fp8_operand &B, void *C, int type,
                            int64_t ldc, bool accumulate, void *ws, hipStream_t st);
 size_t gemm_fp8_workspace(int m, int n, int k);
+// Whether one launch covers the product.
+bool gemm_fp8_fits(int m, int n, int k, int scale_type, int type);
 
 // The same with few tokens, W the operand with the many rows; entry (t, r) of Y at
 // t y_tok + r y_row.

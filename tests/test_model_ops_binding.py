@@ -127,3 +127,35 @@ def test_scratch_of_small_updates():
             for batch in (1, 65535):
                 assert (need(batch, rows, cols, t) <= 256) == small, (t, rows, cols, batch)
         assert need(2, 300, 200, t) > 2 * 2 * 5 * 200 * 200
+
+
+# ---- launches of more threads than one launch has --------------------------------
+
+def test_more_threads_than_a_launch_has():
+    """A launch counts its threads in 32 bits; sizes past that are refused on the host, by the linear layer
+    before its tokens are quantized (the addresses are never read)."""
+    ptr, L, size = 1 << 20, o2m._L, -25
+
+    def operand(**kw):
+        f = dict(values=ptr, ld=16, scales=ptr, s_row=1, s_blk=1 << 31, block=1, format=0, scale_type=0)
+        f.update(kw)
+        return M._Operand(**f)
+    q, tall = operand(), operand(ld=1 << 31)
+
+    def quantize(rows, k, order, ld, Q, Qt):
+        return L.o2m_quantize_fp8(rows, k, ptr, 2, order, ld, Q, Qt, None)
+
+    def gemm(m, n, w, t=2):
+        return L.o2m_gemm_fp8(m, n, 16, w, w, ptr, t, b"R", 1 << 31, 0, ptr, 1 << 62, None)
+
+    def linear(tokens, n, w, t=2):
+        return L.o2m_linear_fp8(tokens, n, 16, ptr, t, 16, w, ptr, 1 << 31, ptr, 1 << 62, None)
+    most = (1 << 31) - 1024
+    assert quantize(1 << 28, 1, b"R", 1, q, None) == size            # 16 blocks of 1 x 128 to 256 threads
+    assert quantize(1 << 30, 1, b"R", 1, operand(block=128), None) == size   # a block of 128 x 128 to 512
+    assert quantize(1 << 30, 1, b"R", 1, operand(values=2 * ptr, scales=2 * ptr), tall) == size
+    assert gemm(5, 1 << 28, q) == size and gemm(1 << 28, 5, q) == size       # 16 rows to 256
+    f32 = operand(scale_type=1)
+    assert gemm(most, 300, f32, 0) == size and gemm(300, most, q, 0) == size   # 128 x 128 at most to 256
+    assert linear(1, 1 << 28, q) == size and linear(1 << 28, 16, q) == size
+    assert linear(200, most, f32, 0) == size   # (the tokens alone would fit)
