@@ -337,8 +337,10 @@ size_t o2m_gemm_fp8_workspace(int m, int n, int k);
 /* The linear layer Y = X W^T: X (tokens x k, of x_type, row-major) is quantized
    to e4m3 in blocks of 1 x 128 with W's kind of scales (as o2m_quantize_fp8
    does) and multiplied with W (n rows of k); Y (tokens x n, row-major) is of
-   x_type.  One launch for few tokens.  Argument errors: -1 tokens, -2 n, -3 k,
-   -4 X, -5 x_type, -6 ldx, -7 W, -8 Y, -9 ldy. */
+   x_type.  One launch for few tokens, the calls that need no workspace: there Y
+   must not share memory with X, which other calls read before they write.
+   Argument errors: -1 tokens, -2 n, -3 k, -4 X, -5 x_type, -6 ldx, -7 W, -8 Y,
+   -9 ldy. */
 o2m_status o2m_linear_fp8(int tokens, int n, int k, const void *X, int x_type, int64_t ldx,
                           const o2m_fp8_operand *W, void *Y, int64_t ldy, void *workspace,
                           size_t workspace_bytes, void *stream);

@@ -45,6 +45,21 @@ bool scales_apart(const o2m_fp8_operand *o, int rows, int k) {
 // Sizes up to here, so that a row past the last tile is still an int.
 constexpr int kMaxSize = 0x7FFFFFFF - 1023;
 
+// `lines` runs of `bytes` bytes, `pitch` apart.
+struct Runs {
+    const void *at;
+    int64_t lines, pitch, bytes;
+};
+// Whether two such sets may share a byte: not if they lie one behind the other, or
+// side by side in rows of one pitch.
+bool may_meet(const Runs &x, const Runs &y) {
+    const int64_t d = static_cast<const char *>(y.at) - static_cast<const char *>(x.at);
+    if (d >= (x.lines - 1) * x.pitch + x.bytes || -d >= (y.lines - 1) * y.pitch + y.bytes) return false;
+    if (x.pitch != y.pitch || x.pitch <= 0) return true;
+    const int64_t in = (d % x.pitch + x.pitch) % x.pitch;
+    return in < x.bytes || x.pitch - in < y.bytes;
+}
+
 o2m_status check_workspace(size_t need, const void *ws, size_t bytes) {
     if (need == 0) return O2M_OK;
     return ws && bytes >= need && aligned(ws, 256) ? O2M_OK : O2M_ERR_WORKSPACE;
@@ -151,7 +166,11 @@ o2m_status o2m_linear_fp8(int tokens, int n, int k, const void *X, int x_type, i
     if (W->ld >= kMaxPitch || round_up64(k, 16) >= kMaxPitch || tokens > kMaxSize || n > kMaxSize) return O2M_ERR_SIZE;
     const o2m_status s = check_workspace(o2m_linear_fp8_workspace(tokens, n, k), workspace, workspace_bytes);
     if (s != O2M_OK) return s;
-    if (linear_is_fused(tokens, k)) return hip_fail(launch_linear_fused(tokens, n, k, X, x_type, ldx, *W, Y, ldy, st));
+    const bool fused = linear_is_fused(tokens, k);
+    const int64_t size = type_bytes(x_type);
+    // (every workgroup reads the tokens, others may have written by then)
+    if (fused && may_meet({X, tokens, ldx * size, k * size}, {Y, tokens, ldy * size, n * size})) return -8;
+    if (fused) return hip_fail(launch_linear_fused(tokens, n, k, X, x_type, ldx, *W, Y, ldy, st));
     // (the product is checked before the tokens are quantized)
     if (!gemm_fp8_fits(tokens, n, k, W->scale_type, x_type)) return O2M_ERR_SIZE;
     const o2m_fp8_operand q = kept_x(tokens, k, W->scale_type, workspace);

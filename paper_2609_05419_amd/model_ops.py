@@ -170,6 +170,27 @@ def _empty(size, dtype, device, stream):
         return torch.empty(size, dtype=dtype, device=device)
 
 
+def _reach(x: torch.Tensor):
+    """First byte of a tensor with entries, and the one behind its last."""
+    at = x.data_ptr()
+    return at, at + x.element_size() * (1 + sum((n - 1) * s for n, s in zip(x.shape, x.stride())))
+
+
+def _shares(x: torch.Tensor, y: torch.Tensor) -> bool:
+    """Whether two tensors reach into one another's memory."""
+    if x.numel() == 0 or y.numel() == 0:
+        return False
+    (a, b), (c, d) = _reach(x), _reach(y)
+    return a < d and c < b
+
+
+def _copy(x: torch.Tensor, stream) -> torch.Tensor:
+    if stream is None:
+        return x.clone()
+    with torch.cuda.stream(stream):
+        return x.clone()
+
+
 def _scratch(nbytes: int, beside: torch.Tensor, stream):
     """(tensor that holds it, address, bytes) of scratch memory on the device of
     ``beside``; torch's blocks are 512-byte aligned."""
@@ -288,7 +309,8 @@ def gemm_fp8(A, B, dtype=torch.bfloat16, out: torch.Tensor | None = None, accumu
 def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The linear layer Y = X W^T: X (tokens x k, row-major) is quantized to e4m3
     in blocks of 1 x 128 with W's kind of scales and multiplied with the operand
-    W (n rows of k); Y (tokens x n, row-major) has X's type."""
+    W (n rows of k); Y (tokens x n, row-major) has X's type.  ``out`` may lie in X's
+    memory."""
     t = _type_of(X, "X")
     w = _operand(W, "W")
     order, ldx = _matrix(X, "X")
@@ -298,6 +320,7 @@ def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None)
         raise ValueError(f"inner dimensions differ: {tuple(X.shape)} and {tuple(W[0].shape)}")
     if order != b"R":
         raise ValueError("X must be row-major")
+    given = out is not None
     if out is None:
         out = _empty((tokens, n), X.dtype, X.device, stream)
         ldy = max(n, 1)
@@ -307,7 +330,11 @@ def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None)
         order, ldy = _matrix(out, "out")
         if order != b"R":
             raise ValueError("out must be row-major")
-    ws, at, nbytes = _scratch(_L.o2m_linear_fp8_workspace(tokens, n, k), out, stream)
+    nbytes = _L.o2m_linear_fp8_workspace(tokens, n, k)
+    if given and nbytes == 0 and _shares(X, out):   # one launch, which writes while it reads
+        X = _copy(X, stream)
+        _, ldx = _matrix(X, "X")
+    ws, at, nbytes = _scratch(nbytes, out, stream)
     _check(_L.o2m_linear_fp8(tokens, n, k, X.data_ptr(), t, ldx, w, out.data_ptr(), ldy, at, nbytes,
                              _stream(stream)), "linear_fp8")
     return out

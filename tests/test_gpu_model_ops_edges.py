@@ -43,3 +43,32 @@ def test_most_small_updates(o2m, steps):  # noqa: F811
     assert torch.cuda.max_memory_allocated() - before <= x.numel() * 4 + (4 << 20)
     for i in (0, 1, 40000, 65534):
         assert torch.equal(x[i], o2m.orthogonalize(g[i], steps=steps))
+
+
+# ---- results in the memory of inputs ------------------------------------------------
+
+@pytest.mark.parametrize("tokens", [1, 3, 16, 40])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_into_its_tokens(o2m, tokens, dtype):  # noqa: F811
+    """The layer's result in its tokens' place, over a part of them, beside them and behind them: as if
+    it were elsewhere, for sizes of one launch and of several."""
+    k, n = 700, 700
+    W = o2m.quantize_fp8(matrix(n, k, 5, spread=0.3), (128, 128))
+    x0 = matrix(tokens, k, 6, dtype, spread=0.3)
+    want = o2m.linear_fp8(x0, W)
+    for first, width in ((0, k), (300, 1000), (k, 2 * k)):   # the output's first column, a row's entries
+        buf = torch.zeros((tokens, width), dtype=dtype, device=DEV)
+        buf[:, :k] = x0
+        out = buf[:, first:first + n]
+        assert o2m.linear_fp8(buf[:, :k], W, out=out) is out
+        assert torch.equal(out, want)
+        assert torch.equal(buf[:, :min(first, k)], x0[:, :min(first, k)])
+    flat = torch.zeros(2 * tokens * k, dtype=dtype, device=DEV)
+    x, out = flat[:tokens * k].view(tokens, k), flat[tokens * k:].view(tokens, n)
+    x.copy_(x0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o2m.linear_fp8(x, W, out=out, stream=side)
+    o2m.linear_fp8(x, W, out=x, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(x, want)

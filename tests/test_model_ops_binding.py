@@ -149,7 +149,7 @@ def test_more_threads_than_a_launch_has():
         return L.o2m_gemm_fp8(m, n, 16, w, w, ptr, t, b"R", 1 << 31, 0, ptr, 1 << 62, None)
 
     def linear(tokens, n, w, t=2):
-        return L.o2m_linear_fp8(tokens, n, 16, ptr, t, 16, w, ptr, 1 << 31, ptr, 1 << 62, None)
+        return L.o2m_linear_fp8(tokens, n, 16, ptr, t, 16, w, 1 << 44, 1 << 31, ptr, 1 << 62, None)
     most = (1 << 31) - 1024
     assert quantize(1 << 28, 1, b"R", 1, q, None) == size            # 16 blocks of 1 x 128 to 256 threads
     assert quantize(1 << 30, 1, b"R", 1, operand(block=128), None) == size   # a block of 128 x 128 to 512
@@ -159,3 +159,25 @@ def test_more_threads_than_a_launch_has():
     assert gemm(most, 300, f32, 0) == size and gemm(300, most, q, 0) == size   # 128 x 128 at most to 256
     assert linear(1, 1 << 28, q) == size and linear(1 << 28, 16, q) == size
     assert linear(200, most, f32, 0) == size   # (the tokens alone would fit)
+
+
+# ---- results in the memory of inputs ---------------------------------------------
+
+@pytest.mark.parametrize("dx,ldx,dy,ldy,n", [
+    (0, 40, 0, 40, 40), (0, 40, 39, 40, 40), (39, 40, 0, 40, 40),       # the same place, the last entry
+    (0, 100, 30, 100, 40), (30, 100, 0, 100, 40), (0, 100, 90, 100, 40),   # rows of one pitch that meet
+    (0, 100, 50, 90, 40)])
+def test_linear_in_one_launch_refuses_its_tokens_memory(dx, ldx, dy, ldy, n):
+    """3 tokens of 40 entries, bf16 (the addresses are never read)."""
+    ptr = 1 << 20
+    w = M._Operand(ptr, 48, ptr, 1, n, 1, 0, 0)
+    assert o2m._L.o2m_linear_fp8_workspace(3, n, 40) == 0
+    assert o2m._L.o2m_linear_fp8(3, n, 40, ptr + 2 * dx, 2, ldx, w, ptr + 2 * dy, ldy, None, 0, None) == -8
+
+
+def test_shared_memory_is_seen():
+    x = torch.zeros(6, 20)
+    for a, b, shares in ((x, x, True), (x[:3], x[3:], False), (x[:3], x[2:], True), (x[5:], x[:5], False),
+                         (x[::2], x[1::2], True), (x[:, :10], x[:, 10:], True), (x[:, :0], x, False),
+                         (x[0:1, :10], x[0:1, 10:], False), (x, x.clone(), False), (x.t(), x, True)):
+        assert M._shares(a, b) == M._shares(b, a) == shares
