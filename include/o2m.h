@@ -359,8 +359,10 @@ size_t o2m_linear_fp8_workspace(int tokens, int n, int k);
    asks for singular values below 4 in every step, which the usual
    coefficients keep far below 2.  A matrix has at most 2^29 entries (its sizes
    rounded up to multiples of 64) and a side of at most 2^21.  Inf or NaN in G
-   gives NaN in the whole matrix.  O must not overlap G, except to be G in the same layout.  Argument
-   errors: -1 batch, -2 rows, -3 cols, -4 G, -5 order_g, -6 ldg, -7 stride_g,
+   gives NaN in the whole matrix.  O may be G in the same layout.  Otherwise a
+   batch of small matrices (those with a workspace of 256 bytes, one launch) must
+   not share memory with its O (-8); other calls read G before they write.
+   Argument errors: -1 batch, -2 rows, -3 cols, -4 G, -5 order_g, -6 ldg, -7 stride_g,
    -8 O, -9 order_o, -10 ldo, -11 stride_o, -12 type, O2M_ERR_STEPS steps,
    coef or eps. */
 o2m_status o2m_orthogonalize(int batch, int rows, int cols, const void *G, char order_g, int64_t ldg,

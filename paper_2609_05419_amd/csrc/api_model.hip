@@ -215,6 +215,23 @@ o2m_status o2m_orthogonalize(int batch, int rows, int cols, const void *G, char 
     if (c > (1 << 21) || (rt * ct) << 12 > (1 << 29) || batch > 65535 || 256 * rt * ct > 0x7FFFFFFF / (int64_t)batch) return O2M_ERR_SIZE;
     const o2m_status s = check_workspace(ortho_workspace(batch, r, c, type), workspace, workspace_bytes);
     if (s != O2M_OK) return s;
+    // Workgroups that have a matrix each finish while others still read theirs.  (Longer
+    // updates, and one matrix alone, are read in full before anything is written.)
+    const bool same = G == O && og == oo && ldg == ldo && stride_g == stride_o;
+    if (batch > 1 && !same && ortho_is_small(r, c, type)) {
+        const int64_t size = type_bytes(type);
+        auto whole = [&](const void *at, char order, int64_t ld, int64_t stride) {
+            const int64_t lines = order == 'R' ? rows : cols, len = order == 'R' ? cols : rows;
+            return Runs{at, batch, stride * size, (ld * (lines - 1) + len) * size};
+        };
+        auto lines = [&](const void *at, char order, int64_t ld, int64_t stride) {
+            return Runs{at, stride / ld * (batch - 1) + (order == 'R' ? rows : cols), ld * size, (order == 'R' ? cols : rows) * size};
+        };
+        const bool one_pitch = ldg == ldo && stride_g % ldg == 0 && stride_o % ldo == 0;
+        if (may_meet(whole(G, og, ldg, stride_g), whole(O, oo, ldo, stride_o)) &&
+            !(one_pitch && !may_meet(lines(G, og, ldg, stride_g), lines(O, oo, ldo, stride_o))))
+            return -8;
+    }
     OrthoArgs a;
     a.batch = batch;
     a.rows = r;

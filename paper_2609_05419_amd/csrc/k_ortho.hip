@@ -683,17 +683,19 @@ hipError_t run_ortho(const OrthoArgs &o, const Buffers &b, hipStream_t st) {
 
 }  // namespace
 
+bool ortho_is_small(int rows, int cols, int type) { return ortho_fits_lds(rows, cols, split_of(type)); }
+
 // Small matrices stay in LDS: 256 bytes, which nothing uses, so that a caller passes
 // a workspace for every size.
 size_t ortho_workspace(int batch, int rows, int cols, int type) {
-    if (ortho_is_small(rows, cols, split_of(type))) return 256;
+    if (ortho_is_small(rows, cols, type)) return 256;
     return carve(batch, rows, cols, split_of(type), nullptr, nullptr);
 }
 
 hipError_t launch_ortho(const OrthoArgs &o, void *ws, hipStream_t st) {
     Buffers b;
     const bool split = split_of(o.type);
-    if (ortho_is_small(o.rows, o.cols, split)) return launch_ortho_small(o, split, st);
+    if (ortho_is_small(o.rows, o.cols, o.type)) return launch_ortho_small(o, split, st);
     carve(o.batch, o.rows, o.cols, split, ws, &b);
     return split ? run_ortho<true>(o, b, st) : run_ortho<false>(o, b, st);
 }

@@ -230,7 +230,7 @@ int64_t lds_bytes(int r, int c, bool split) {
 }  // namespace
 
 // Matrices that fit, whose products are one round of the waves.
-bool ortho_is_small(int r, int c, bool split) {
+bool ortho_fits_lds(int r, int c, bool split) {
     const int64_t rt = ceil_div(r, 32), ct = ceil_div(c, 32);
     return rt * ct <= kWaves && lds_bytes(r, c, split) <= kLdsBytes;
 }

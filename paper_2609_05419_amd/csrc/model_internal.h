@@ -54,6 +54,8 @@ struct OrthoArgs {
     double eps;
 };
 size_t ortho_workspace(int batch, int rows, int cols, int type);
+// Whether the whole update is one launch, of a workgroup per matrix.
+bool ortho_is_small(int rows, int cols, int type);
 hipError_t launch_ortho(const OrthoArgs &g, void *ws, hipStream_t st);
 
 // Zero entries (i, j) of C at i + j ldc, of `size` bytes.

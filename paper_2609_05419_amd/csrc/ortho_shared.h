@@ -39,7 +39,7 @@ struct Lines {
 
 // The whole update of matrices that fit into LDS, one workgroup each
 // (k_ortho_small.hip).
-bool ortho_is_small(int r, int c, bool split);
+bool ortho_fits_lds(int r, int c, bool split);
 hipError_t launch_ortho_small(const OrthoArgs &o, bool split, hipStream_t st);
 
 }  // namespace o2m

@@ -66,6 +66,7 @@ _SCALE_KINDS = {_SCALE_DTYPES["pow2"]: 0, torch.uint8: 0, torch.float32: 1}
 BLOCK = 128
 _LARGEST = (1 << 31) - 1   # what the C calls' sizes hold: ctypes would drop the bits above
 _ERR_STEPS, _MOST_STEPS = -28, 64
+_SMALL_UPDATE = 256        # scratch bytes of an update in one launch
 
 
 class Fp8Operand(NamedTuple):
@@ -373,7 +374,7 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750
     float32, float16 or bfloat16): X = G / (||G|| + eps) in the Frobenius norm, then
     ``steps`` times X <- a X + (b A + c A^2) X with A = X X^T on the shorter side.
     ``coefficients``: (a, b, c), or one such triple for each step.  The result
-    (or ``out``) has G's shape and type."""
+    (or ``out``, which may lie in G's memory) has G's shape and type."""
     t = _type_of(G, "G")
     if G.dim() not in (2, 3):
         raise ValueError(f"G must be a matrix or a batch of matrices, got {G.dim()} dimensions")
@@ -384,6 +385,7 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750
     rows, cols = G.shape[-2:]
     batch = G.size(0) if G.dim() == 3 else 1
     og, ldg = _order(rows, cols, G.stride(-2), G.stride(-1), "G")
+    given = out is not None
     if out is None:
         if og == b"R":
             out = _empty(tuple(G.shape), G.dtype, G.device, stream)
@@ -399,7 +401,12 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750
     if len(flat) != 3 * steps:
         raise ValueError(f"coefficients must be one triple or {steps} of them")
     coef = (ctypes.c_double * max(len(flat), 1))(*flat)
-    ws, at, nbytes = _scratch(_L.o2m_orthogonalize_workspace(batch, rows, cols, t), out, stream)
+    nbytes = _L.o2m_orthogonalize_workspace(batch, rows, cols, t)
+    if (given and batch > 1 and nbytes <= _SMALL_UPDATE and _shares(G, out)
+            and (G.data_ptr() != out.data_ptr() or G.stride() != out.stride())):
+        G = _copy(G, stream)   # one launch, which writes matrices while it reads others
+        og, ldg = _order(rows, cols, G.stride(-2), G.stride(-1), "G")
+    ws, at, nbytes = _scratch(nbytes, out, stream)
     _check(_L.o2m_orthogonalize(batch, rows, cols, G.data_ptr(), og, ldg, G.stride(0) if G.dim() == 3 else 0,
                                 out.data_ptr(), oo, ldo, out.stride(0) if G.dim() == 3 else 0, t, steps,
                                 ctypes.addressof(coef), eps, at, nbytes, _stream(stream)), "orthogonalize")

@@ -72,3 +72,28 @@ def test_linear_into_its_tokens(o2m, tokens, dtype):  # noqa: F811
     o2m.linear_fp8(x, W, out=x, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(x, want)
+
+
+@pytest.mark.parametrize("n", [24, 70, 300])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_updates_into_their_own_memory(o2m, n, dtype):  # noqa: F811
+    """A batch into its own memory in the same layout, across, a matrix further on, and beside itself in
+    rows of one pitch: as if it were elsewhere, for sizes of one launch and of several."""
+    b = 40
+    g0 = torch.stack([matrix(n, n, 40 + i, dtype, spread=0.3) for i in range(b)])
+    want = o2m.orthogonalize(g0)
+    for into in (lambda g: g, lambda g: g.transpose(1, 2)):
+        g = g0.clone()
+        out = into(g)
+        assert o2m.orthogonalize(g, out=out) is out
+        assert torch.equal(out, want)
+    buf = torch.zeros((b + 1, n, n), dtype=dtype, device=DEV)
+    for g, out in ((buf[:b], buf[1:]), (buf[1:], buf[:b])):
+        g.copy_(g0)
+        assert torch.equal(o2m.orthogonalize(g, out=out), want)
+    for first in (n, n // 2):
+        wide = torch.zeros((b, n, 2 * n), dtype=dtype, device=DEV)
+        g, out = wide[:, :, :n], wide[:, :, first:first + n]
+        g.copy_(g0)
+        assert torch.equal(o2m.orthogonalize(g, out=out), want)
+        assert torch.equal(wide[:, :, :first], g0[:, :, :first])

@@ -1,5 +1,6 @@
 """What the binding of the products of trained models checks before it allocates
 or calls anything (no GPU, and no memory behind the large shapes)."""
+import ctypes
 import os
 import subprocess
 import sys
@@ -181,3 +182,18 @@ def test_shared_memory_is_seen():
                          (x[::2], x[1::2], True), (x[:, :10], x[:, 10:], True), (x[:, :0], x, False),
                          (x[0:1, :10], x[0:1, 10:], False), (x, x.clone(), False), (x.t(), x, True)):
         assert M._shares(a, b) == M._shares(b, a) == shares
+
+
+@pytest.mark.parametrize("dg,og,ldg,sg,do,oo,ldo,so", [
+    (0, b"R", 9, 54, 0, b"C", 6, 54),              # in place, but across
+    (0, b"R", 9, 54, 5, b"R", 9, 54), (54, b"R", 9, 54, 0, b"R", 9, 54),   # a part of a matrix, or a whole one, on
+    (0, b"R", 9, 0, 53, b"R", 9, 54),              # one G for all
+    (0, b"R", 20, 240, 3, b"R", 20, 240),          # rows of one pitch that meet
+    (0, b"R", 20, 240, 12, b"R", 20, 241)])
+def test_a_batch_of_small_updates_refuses_its_own_memory(dg, og, ldg, sg, do, oo, ldo, so):
+    """2 matrices of 6 x 9, fp32 (the addresses are never read)."""
+    ptr, L = 1 << 20, o2m._L
+    assert L.o2m_orthogonalize_workspace(2, 6, 9, 0) == M._SMALL_UPDATE
+    coef = (ctypes.c_double * 3)(1.0, 1.0, 1.0)
+    assert L.o2m_orthogonalize(2, 6, 9, ptr + 4 * dg, og, ldg, sg, ptr + 4 * do, oo, ldo, so, 0, 1,
+                               ctypes.addressof(coef), 0.0, ptr, 256, None) == -8
