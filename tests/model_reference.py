@@ -154,3 +154,46 @@ def orthogonalize_bound(sigma, cols, parts, dtype, steps=5, coef=COEF):
         d_x = top * d_b + u * frob(sigma[t + 1]) + 2 * (r + 2) * fp * frob(held_b) * frob(s)
         err = gain * err + d_x
     return err + half_step(dtype) * frob(sigma[-1])
+
+
+def orthogonalize_step(x, coef):
+    """One step on one float64 matrix."""
+    a, b, c = coef
+    if x.shape[0] > x.shape[1]:
+        return orthogonalize_step(x.T, coef).T
+    t = x @ x.T
+    return a * x + (b * t + c * (t @ t)) @ x
+
+
+def orthogonalize_step_bound(x, coef, parts, dtype):
+    """Bound of the Frobenius norm of what one step may be off, given the result x (float64) of
+    the steps before, rounded to dtype.  The step itself starts from the same numbers in fp32, held in one
+    or two fp16 parts, so its start is off x by both roundings; a start that is off by e gives a
+    result that is off by at most e max |p'| over the singular values, p(s) = a s + b s^3 + c s^5.  Then
+      - A = X X^T, A^2 and B X are summed in fp32: of n terms every one passes a rounding (of at most one
+        unit, 2^-23) for each 32 terms of each pass (three with two parts), 32 within such a run and 16 where
+        splits are joined, so a sum is off by that of the sum of its terms' magnitudes; with two parts the
+        products of the low ones, each below 2^-11 of its number, are left out;
+      - A, B = a + b A + c A^2 and X are held, and B is added up from three terms in fp32.
+    fp16 numbers end at 2^-24 of X 2^14, A 2^11, B 2^6, so each held entry may be off by half of
+    that too.  1.05: what is of second order."""
+    if x.shape[0] > x.shape[1]:
+        x = x.T
+    (r, c), (a, b, k5) = x.shape, coef
+    norm = np.linalg.norm
+    one = half_step(torch.float16)
+    u, low, passes = (one, 0.0, 1) if parts == 1 else (one * one, one * one, 3)
+    sums = lambda n: (passes * -(-n // 32) + 48) * 2.0 ** -23 + low  # noqa: E731
+    tiny = {torch.float32: 2.0 ** -150, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}[dtype]
+    s = np.linalg.svd(x, compute_uv=False)
+    grid = np.linspace(0.0, 1.01 * s[0], 4001)
+    gain = np.abs(a + 3 * b * grid ** 2 + 5 * k5 * grid ** 4).max()
+    start = (u + half_step(dtype)) * norm(x) + (2.0 ** -39 + tiny) * math.sqrt(r * c)
+    t = x @ x.T
+    held_b = a * np.eye(r) + b * t + k5 * (t @ t)
+    d_a = u * norm(t) + sums(c) * norm(np.abs(x) @ np.abs(x).T) + 2.0 ** -36 * r
+    d_b = ((abs(b) + 2 * abs(k5) * s[0] ** 2) * d_a + abs(k5) * sums(r) * norm(np.abs(t) @ np.abs(t)) + 2.0 ** -31 * r
+           + u * norm(held_b) + 4 * 2.0 ** -24 * (abs(a) * math.sqrt(r) + abs(b) * norm(t) + abs(k5) * norm(t @ t)))
+    exact = orthogonalize_step(x, coef)
+    d_x = s[0] * d_b + sums(r) * norm(np.abs(held_b) @ np.abs(x))
+    return 1.05 * (gain * start + d_x) + half_step(dtype) * norm(exact) + tiny * math.sqrt(r * c)

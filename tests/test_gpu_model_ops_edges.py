@@ -97,3 +97,37 @@ def test_updates_into_their_own_memory(o2m, n, dtype):  # noqa: F811
         g.copy_(g0)
         assert torch.equal(o2m.orthogonalize(g, out=out), want)
         assert torch.equal(wide[:, :, :first], g0[:, :, :first])
+
+
+# ---- the update step by step ----------------------------------------------------------
+
+TRIPLES = [(3.4445, -4.7750, 2.0315), (3.0, -3.2, 1.2), (2.5, -2.0, 0.5), (2.0, -1.5, 0.5), (1.875, -1.25, 0.375)]
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 200), (96, 80), (33, 90), (64, 64), (60, 150), (100, 140), (130, 129),
+                                       (64, 500), (513, 300), (900, 1000)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_update_step_by_step(o2m, rows, cols, dtype):  # noqa: F811
+    """The update of no, one, .. five steps, each against one step of the definition on the result of the
+    one before, within a bound that is far below the result (test_update_bound.py): matrices of one
+    launch and of several, coefficients of their own for each step."""
+    parts = 1 if dtype == torch.bfloat16 else 2
+    g = torch.stack([matrix(rows, cols, 21 + i, dtype, spread=0.3) for i in range(2)])
+    x = g[1].double().cpu().numpy()
+    x = x / (np.linalg.norm(x) + 1e-7)
+    got = o2m.orthogonalize(g, steps=0)[1].double().cpu().numpy()
+    one = R.half_step(torch.float16)
+    u = (one if parts == 1 else one * one) + R.half_step(dtype) + 2.0 ** -23
+    tiny = 2.0 ** -39 + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+    assert (np.abs(got - x) <= 1.01 * u * np.abs(x) + tiny).all()
+    for t, coef in enumerate(TRIPLES):
+        print("step", t + 1, rows, cols, dtype, flush=True)
+        x = got
+        got = o2m.orthogonalize(g, steps=t + 1, coefficients=TRIPLES[:t + 1])[1].double().cpu().numpy()
+        exact = R.orthogonalize_step(x, coef)
+        bound = R.orthogonalize_step_bound(x, coef, parts, dtype)
+        off = np.linalg.norm(got - exact)
+        assert off <= bound, (t, off / bound, bound / np.linalg.norm(exact))
+    # one triple for all steps
+    assert torch.equal(o2m.orthogonalize(g, steps=3, coefficients=TRIPLES[1]),
+                       o2m.orthogonalize(g, steps=3, coefficients=[TRIPLES[1]] * 3))
