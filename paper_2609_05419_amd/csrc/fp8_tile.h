@@ -3,18 +3,11 @@
 #pragma once
 
 #include "fp8_operand.h"
+#include "fp8_plan.h"
 #include "mfma_pipe.h"
 #include "tile_schedule.h"
 
 namespace o2m {
-
-// How a block's products are added up.
-enum Sum {
-    kScaled,       // 8-bit MFMA with power-of-two scales
-    kPartial,      // 8-bit MFMA, then fp32 scales
-    kWide,         // fp16 MFMA, then fp32 scales
-    kWideScaled,   // bf16 MFMA of values scaled by powers of two as they are widened
-};
 
 // C = A B^T, entry (i, j) at C[i ldc + j].
 struct Fp8Args {
@@ -241,7 +234,6 @@ hipError_t launch_tile(Fp8Args &g, hipStream_t st) {
 // and 256 x 128), 128 x 128 by 4 (two workgroups per CU), 64 x 64 by 4 (four; two with
 // three stages on their way each were never faster: 1537 x 1283 x 2051, 525 tiles, 22
 // against 17 us).
-enum TileSize { k256, k256x128, k128, k64 };
 template <Sum SUM, int FA, int FB, bool WB>
 hipError_t launch_sizes(Fp8Args &g, TileSize size, hipStream_t st) {
     switch (size) {

@@ -8,14 +8,10 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "blocks.h"
 #include "o2m.h"
 
 namespace o2m {
-
-constexpr int kBlockK = 128;   // entries of a block along the inner dimension
-
-inline int64_t ceil_div(int64_t x, int64_t q) { return (x + q - 1) / q; }
-inline int64_t round_up64(int64_t x, int64_t q) { return ceil_div(x, q) * q; }
 
 // The runtime counts a launch's threads in 32 bits.
 inline bool launch_fits(int64_t groups, int threads) { return groups * threads <= 0xFFFFFFFFLL; }

@@ -5,6 +5,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 import model_reference as R  # noqa: E402
+from fp8_shapes import SPLIT, SPLIT_LINEAR  # noqa: E402
 from test_gpu_model_ops import DEV, E4M3, TYPES, matrix, o2m, padded_operand  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
@@ -131,3 +132,60 @@ def test_update_step_by_step(o2m, rows, cols, dtype):  # noqa: F811
     # one triple for all steps
     assert torch.equal(o2m.orthogonalize(g, steps=3, coefficients=TRIPLES[1]),
                        o2m.orthogonalize(g, steps=3, coefficients=[TRIPLES[1]] * 3))
+
+
+# ---- products split along k (test_fp8_plan.py: that they are) ----------------------------
+
+@pytest.mark.parametrize("m,n,k,splits", SPLIT)
+@pytest.mark.parametrize("scales", ["pow2", "float32"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gemm_in_splits(o2m, m, n, k, splits, scales, dtype):  # noqa: F811
+    """Sums of splits joined: either order of the result, fresh or added to, rows of odd pitch behind which
+    nothing changes, a row of NaN and a column of it."""
+    a, b = matrix(m, k, 71, spread=0.5), matrix(n, k, 72, spread=0.5)
+    a[m // 2, k // 3], b[n - 1, k - 1] = float("nan"), float("inf")
+    A, _ = padded_operand(o2m, a, 1, E4M3, scales)
+    B = o2m.quantize_fp8(b, (128, 128), R.E5M2 if m % 2 else E4M3, scales)
+    print("split", m, n, k, splits, scales, dtype, flush=True)
+    want = (R.values64(A, 1), R.values64(B, 128), dtype)
+    C = o2m.gemm_fp8(A, B, dtype=dtype)
+    R.check_product(C, *want)
+    for order in ("row", "col"):
+        for add in (False, True):
+            buf = torch.full((m + 3, n + 5) if order == "row" else (n + 3, m + 5), 7.0, dtype=dtype, device=DEV)
+            out = buf[1:1 + m, 2:2 + n] if order == "row" else buf[1:1 + n, 2:2 + m].t()
+            assert o2m.gemm_fp8(A, B, out=out, accumulate=add) is out
+            R.check_product(out, *want, 7.0 * np.ones((m, n)) if add else None)
+            if order == "row" and not add:
+                assert torch.equal(out.contiguous().view(torch.uint8), C.view(torch.uint8))   # NaN as well
+            out.fill_(7.0)
+            assert (buf == 7.0).all()
+
+
+@pytest.mark.parametrize("tokens,n,k", SPLIT_LINEAR)
+@pytest.mark.parametrize("scales", ["pow2", "float32"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_in_splits(o2m, tokens, n, k, scales, dtype):  # noqa: F811
+    """The scratch memory holds the quantized tokens and, behind them, the splits' sums."""
+    x = matrix(tokens, k, 73, dtype, spread=0.5)
+    W, _ = padded_operand(o2m, matrix(n, k, 74, spread=0.5), 128, E4M3, scales)
+    buf = torch.full((tokens + 1, n + 3), 7.0, dtype=dtype, device=DEV)
+    y = o2m.linear_fp8(x, W, out=buf[:tokens, :n])
+    q, s = R.quantize(x.float().cpu().numpy(), 1, E4M3, scales)
+    R.check_product(y, q * R.spread(s, 1, tokens, k), R.values64(W, 128), dtype)
+    assert (buf[:, n:] == 7).all() and (buf[tokens:] == 7).all()
+
+
+@pytest.mark.parametrize("scales,fmt", [("pow2", E4M3), ("float32", R.E5M2)])
+def test_weight_gradient_over_many_tokens(o2m, scales, fmt):  # noqa: F811
+    """dW of 10007 tokens, in splits, added to the gradient of the batch before."""
+    tokens, n, k = 10007, 99, 131
+    _, xt = o2m.quantize_fp8_pair(matrix(tokens, k, 75, torch.bfloat16, spread=0.3), scales=scales)
+    _, wt = o2m.quantize_fp8_pair(matrix(n, k, 76, spread=0.3), (128, 128), scales=scales)
+    dw = None
+    for i in range(3):
+        dy = matrix(tokens, n, 77 + i, torch.bfloat16, spread=0.3)
+        first = None if dw is None else dw.double().cpu().numpy()
+        _, dw = o2m.linear_fp8_backward(dy, xt, wt, dtype=fmt, dW=dw, accumulate=dw is not None)
+        qt, st = R.quantize(dy.float().cpu().numpy().T, 1, fmt, scales)
+        R.check_product(dw, qt * R.spread(st, 1, n, tokens), R.values64(xt, 1), torch.float32, first)
