@@ -271,6 +271,12 @@ o2m_status zgemm_2m_residues_ex(int m, int n, int k, const double *A, int lda, c
  *     the call uses until the stream has passed it.  Calls that may overlap, and
  *     graphs that may be replayed at the same time, need one each;
  *   - no call allocates, so each can be captured into a graph at any time.
+ *
+ * Outputs and workspaces share no memory with inputs, except where a call says that
+ * they may. Sizes past what a call's kernels cover are refused with O2M_ERR_SIZE:
+ * rows, tokens, m and n reach 2^31 - 1024 at most, and a launch 2^32 - 1 threads,
+ * which is below 2^28 blocks of 1 x 128 or 2^23 of 128 x 128 to be quantized, and
+ * below 2^28 rows beside up to 32 of the other operand, some 2^29 beside up to 128.
  * ------------------------------------------------------------------------ */
 
 /* element types of unquantized matrices */
@@ -291,7 +297,8 @@ o2m_status zgemm_2m_residues_ex(int m, int n, int k, const double *A, int lda, c
    ld, with values 16-byte aligned and ld a multiple of 16, at least k.  The bytes
    of a row past k are neither used nor written.  The value of entry (r, j) is
    its 8-bit number times the scale of block (r / block, j / 128), which is
-   element (r / block) s_row + (j / 128) s_blk of scales. */
+   element (r / block) s_row + (j / 128) s_blk of scales.  Products take ld below
+   2^23, so k up to 2^23 - 16 (O2M_ERR_SIZE). */
 typedef struct {
     void *values;
     int64_t ld;
@@ -312,23 +319,26 @@ typedef struct {
    (s = 1 when amax = 0), and an entry becomes fl(x fl(1/s)), limited to
    [-F, F] and rounded to the nearest 8-bit number, ties to even; Inf and NaN
    become NaN.  The blocks at the edges are shorter, nothing is written past
-   them.  The scales of an operand have to lie apart, and Q and Qt too.  Argument errors: -1 rows, -2 k, -3 X, -4 x_type, -5 x_order, -6 ldx,
-   -7 Q, -8 Qt. */
+   them.  The scales of an operand have to lie apart, and Q and Qt too.  Argument
+   errors: -1 rows, -2 k, -3 X, -4 x_type, -5 x_order, -6 ldx, -7 Q, -8 Qt. */
 o2m_status o2m_quantize_fp8(int rows, int k, const void *X, int x_type, char x_order, int64_t ldx,
                             const o2m_fp8_operand *Q, const o2m_fp8_operand *Qt, void *stream);
 
 /* C = A B^T for 8-bit operands A (m rows of k) and B (n rows of k) of the same
-   kind of scales and any formats and blocks, rounded once to c_type.  For
-   fp32 results the products are exact and summed in fp32.  For 16-bit ones they are
-   summed by the 8-bit matrix unit, which adds 8 neighbouring products (k = 8 t
-   .. 8 t + 7) to within 2^-13 of the largest of them each, and these sums in
-   fp32: some 2e-5 of the result's norm, far below its rounding.  Scaled
-   entries, the products of two blocks' scales, and sums have to stay within the
-   range of normal fp32 numbers (smaller ones may count as zeros).  accumulate !=
-   0: C += A B^T, the sum rounded once.  c_order 'R': entry (i, j) at C[i ldc + j],
-   'C': at C[i + j ldc].  Rows holding NaN give NaN.  k == 0: C is set to zero (accumulate: left as it is).  Every run
-   gives the same bits.  Argument errors: -1 m, -2 n, -3 k, -4 A, -5 B, -6 C,
-   -7 c_type, -8 c_order, -9 ldc. */
+   kind of scales and any formats and blocks, rounded once to c_type. For fp32 results
+   the products are exact and summed in fp32. For 16-bit ones they are summed by the
+   8-bit matrix unit, which adds 8 neighbouring products (k = 8 t .. 8 t + 7) cut
+   off 13 bits below the exponent of the largest of them, and these sums in fp32. On
+   matrices whose entries are of like size that is some 2e-5 of the result's norm,
+   far below its rounding. What holds for every entry, besides its rounding, is 2^-10 of the
+   sum over t of max |A[i, k]| max |B[j, k]| in the group: where large products of different
+   groups cancel, that is what is left of them, and a c_type of fp32 is the way to
+   more. Scaled entries, the products of two blocks' scales, and sums have to stay
+   within the range of normal fp32 numbers (smaller ones may count as zeros).
+   accumulate != 0: C += A B^T, the sum rounded once. c_order 'R': entry (i, j) at
+   C[i ldc + j], 'C': at C[i + j ldc]. Rows holding NaN give NaN. k == 0: C is set
+   to zero (accumulate: left as it is). Every run gives the same bits. Argument
+   errors: -1 m, -2 n, -3 k, -4 A, -5 B, -6 C, -7 c_type, -8 c_order, -9 ldc. */
 o2m_status o2m_gemm_fp8(int m, int n, int k, const o2m_fp8_operand *A, const o2m_fp8_operand *B, void *C,
                         int c_type, char c_order, int64_t ldc, int accumulate, void *workspace,
                         size_t workspace_bytes, void *stream);
@@ -353,17 +363,20 @@ size_t o2m_linear_fp8_workspace(int tokens, int n, int k);
    (a, b, c) = coef[3 t .. 3 t + 2] in step t (host memory), and X is written to
    O, of the same type; transposed where rows > cols, which is the same X.
    order 'R': entry (i, j) at i ld + j, 'C': at i + j ld, for G and O each.  The
-   norm is summed in fp64 and products in fp32; between products bf16 matrices
-   are held in fp16 with one power-of-two scale (11 bits, 3 more than the
-   result), fp32 and fp16 ones in two fp16 parts (22 bits).  The held range
-   asks for singular values below 4 in every step, which the usual
-   coefficients keep far below 2.  A matrix has at most 2^29 entries (its sizes
-   rounded up to multiples of 64) and a side of at most 2^21.  Inf or NaN in G
-   gives NaN in the whole matrix.  O may be G in the same layout.  Otherwise a
-   batch of small matrices (those with a workspace of 256 bytes, one launch) must
-   not share memory with its O (-8); other calls read G before they write.
-   Argument errors: -1 batch, -2 rows, -3 cols, -4 G, -5 order_g, -6 ldg, -7 stride_g,
-   -8 O, -9 order_o, -10 ldo, -11 stride_o, -12 type, O2M_ERR_STEPS steps,
+   norm is summed in fp64 and products in fp32; between products bf16 matrices are held
+   in fp16 with one power-of-two scale (11 bits, 3 more than the result), fp32 and
+   fp16 ones in two fp16 parts (22 bits): a bf16 matrix of which more is wanted goes
+   in and out as fp32. The held range asks for singular values s below 4 and |a + b
+   s^2 + c s^4| below 1000 in every step, which the usual coefficients keep far
+   below 2 and 4, and an entry of X is held to within 2^-39 at best: where ||G|| is
+   far below eps, X is small and has fewer bits. A matrix has at most 2^29 entries
+   (its sizes rounded up to multiples of 64) and a side of at most 2^21, a batch at
+   most 65535 matrices and less than 2^23 tiles of 64 x 64 in all (O2M_ERR_SIZE).
+   Inf or NaN in G gives NaN in the whole matrix. O may be G in the same layout.
+   Otherwise a batch of small matrices (those with a workspace of 256 bytes, one
+   launch) must not share memory with its O (-8); other calls read G before they
+   write. Argument errors: -1 batch, -2 rows, -3 cols, -4 G, -5 order_g, -6 ldg, -7
+   stride_g, -8 O, -9 order_o, -10 ldo, -11 stride_o, -12 type, O2M_ERR_STEPS steps,
    coef or eps. */
 o2m_status o2m_orthogonalize(int batch, int rows, int cols, const void *G, char order_g, int64_t ldg,
                              int64_t stride_g, void *O, char order_o, int64_t ldo, int64_t stride_o, int type,

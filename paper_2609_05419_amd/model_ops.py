@@ -279,9 +279,14 @@ def quantize_fp8_pair(X: torch.Tensor, block=(1, 128), dtype=_E4M3, scales: str 
 def gemm_fp8(A, B, dtype=torch.bfloat16, out: torch.Tensor | None = None, accumulate: bool = False,
              stream=None) -> torch.Tensor:
     """C = A B^T for 8-bit operands A (m rows of k) and B (n rows of k) of one
-    kind of scales and any formats and blocks; summed in fp32, rounded once to
-    ``dtype`` (or that of ``out``, which may be row-major or column-major).
-    ``accumulate``: out += A B^T, rounded once."""
+    kind of scales and any formats and blocks, rounded once to ``dtype`` (or that of
+    ``out``, which may be row-major or column-major).  float32 results: exact
+    products summed in fp32.  16-bit ones: 8 neighbouring products at a time are
+    added with 13 bits below the largest, these sums in fp32; some 2e-5 of the
+    result's norm where entries are of like size, but where large products cancel,
+    2^-10 of them may be left in an entry, and ``dtype=torch.float32`` is the way to
+    more.  Products of two blocks' scales have to stay within the range of normal
+    fp32 numbers.  ``accumulate``: out += A B^T, rounded once."""
     a, b = _operand(A, "A"), _operand(B, "B")
     m, k = A[0].shape
     n = B[0].size(0)
@@ -310,8 +315,9 @@ def gemm_fp8(A, B, dtype=torch.bfloat16, out: torch.Tensor | None = None, accumu
 def linear_fp8(X: torch.Tensor, W, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The linear layer Y = X W^T: X (tokens x k, row-major) is quantized to e4m3
     in blocks of 1 x 128 with W's kind of scales and multiplied with the operand
-    W (n rows of k); Y (tokens x n, row-major) has X's type.  ``out`` may lie in X's
-    memory."""
+    W (n rows of k); Y (tokens x n, row-major) has X's type, which decides how
+    products are summed (gemm_fp8: ``X.float()`` for the most).  ``out`` may lie in
+    X's memory."""
     t = _type_of(X, "X")
     w = _operand(W, "W")
     order, ldx = _matrix(X, "X")
@@ -374,7 +380,9 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=(3.4445, -4.7750
     float32, float16 or bfloat16): X = G / (||G|| + eps) in the Frobenius norm, then
     ``steps`` times X <- a X + (b A + c A^2) X with A = X X^T on the shorter side.
     ``coefficients``: (a, b, c), or one such triple for each step.  The result
-    (or ``out``, which may lie in G's memory) has G's shape and type."""
+    (or ``out``, which may lie in G's memory) has G's shape and type.  Between
+    products a bfloat16 matrix is held in 11 bits, others in 22 (``G.float()`` gives a
+    bfloat16 update that precision); singular values have to stay below 4."""
     t = _type_of(G, "G")
     if G.dim() not in (2, 3):
         raise ValueError(f"G must be a matrix or a batch of matrices, got {G.dim()} dimensions")
