@@ -189,3 +189,17 @@ def test_weight_gradient_over_many_tokens(o2m, scales, fmt):  # noqa: F811
         _, dw = o2m.linear_fp8_backward(dy, xt, wt, dtype=fmt, dW=dw, accumulate=dw is not None)
         qt, st = R.quantize(dy.float().cpu().numpy().T, 1, fmt, scales)
         R.check_product(dw, qt * R.spread(st, 1, n, tokens), R.values64(xt, 1), torch.float32, first)
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 90, 512), (70, 90, 512), (301, 299, 8200), (1900, 2100, 512), (3700, 3600, 400)])
+@pytest.mark.parametrize("scales", ["pow2", "float32"])
+def test_gemm_of_cancelling_channels(o2m, m, n, k, scales):  # noqa: F811
+    """Two outlier channels in different groups of 8 whose products cancel exactly: what is left is the
+    sum of the small ones, each entry within the bound that the largest of every group gives for 16-bit
+    results, and within fp32's for fp32 ones."""
+    a, b = matrix(m, k, 81, spread=0.3), matrix(n, k, 82, spread=0.3)
+    a[:, 17], a[:, k - 3] = 256.0, 256.0
+    b[:, 17], b[:, k - 3] = 256.0, -256.0
+    A, B = o2m.quantize_fp8(a, scales=scales), o2m.quantize_fp8(b, scales=scales)
+    for dtype in TYPES:
+        R.check_product(o2m.gemm_fp8(A, B, dtype=dtype), R.values64(A, 1), R.values64(B, 1), dtype)
