@@ -372,7 +372,8 @@ size_t o2m_linear_fp8_workspace(int tokens, int n, int k);
    far below eps, X is small and has fewer bits. A matrix has at most 2^29 entries
    (its sizes rounded up to multiples of 64) and a side of at most 2^21, a batch at
    most 65535 matrices and less than 2^23 tiles of 64 x 64 in all (O2M_ERR_SIZE).
-   Inf or NaN in G gives NaN in the whole matrix. O may be G in the same layout.
+   Inf or NaN in G gives NaN in the whole matrix. The matrices of O lie one behind
+   the other or side by side (stride_o within ldo). O may be G in the same layout.
    Otherwise a batch of small matrices (those with a workspace of 256 bytes, one
    launch) must not share memory with its O (-8); other calls read G before they
    write. Argument errors: -1 batch, -2 rows, -3 cols, -4 G, -5 order_g, -6 ldg, -7

@@ -201,8 +201,11 @@ o2m_status o2m_orthogonalize(int batch, int rows, int cols, const void *G, char 
     if (any && (!O || !aligned(O, type_bytes(type)))) return -8;
     if (!oo) return -9;
     if (ldo < (oo == 'R' ? cols : rows) || ldo < 1) return -10;
-    // matrices of one batch must not share entries
-    if (stride_o < 0 || (any && batch > 1 && stride_o < ldo * (int64_t)((oo == 'R' ? rows : cols) - 1) + (oo == 'R' ? cols : rows)))
+    // the matrices of a batch must not share entries: they lie one behind the other, or side by side
+    // within a row of ldo
+    const int64_t lines_o = oo == 'R' ? rows : cols, len_o = oo == 'R' ? cols : rows;
+    if (stride_o < 0 || (any && batch > 1 && stride_o < ldo * (lines_o - 1) + len_o &&
+                         (stride_o < len_o || ldo < stride_o * (batch - 1) + len_o)))
         return -11;
     if (steps < 0 || steps > 64 || (steps > 0 && !coef) || !(eps >= 0.0) || !isfinite(eps)) return O2M_ERR_STEPS;
     for (int i = 0; i < 3 * steps; ++i)

@@ -136,17 +136,14 @@ def test_update_step_by_step(o2m, rows, cols, dtype):  # noqa: F811
 
 # ---- products split along k (test_fp8_plan.py: that they are) ----------------------------
 
-@pytest.mark.parametrize("m,n,k,splits", SPLIT)
-@pytest.mark.parametrize("scales", ["pow2", "float32"])
-@pytest.mark.parametrize("dtype", TYPES)
-def test_gemm_in_splits(o2m, m, n, k, splits, scales, dtype):  # noqa: F811
-    """Sums of splits joined: either order of the result, fresh or added to, rows of odd pitch behind which
-    nothing changes, a row of NaN and a column of it."""
+def check_outputs(o2m, m, n, k, scales, dtype):  # noqa: F811
+    """Either order of the result, fresh or added to, rows of odd pitch behind which nothing changes, a row
+    of NaN and a column of it."""
     a, b = matrix(m, k, 71, spread=0.5), matrix(n, k, 72, spread=0.5)
     a[m // 2, k // 3], b[n - 1, k - 1] = float("nan"), float("inf")
     A, _ = padded_operand(o2m, a, 1, E4M3, scales)
     B = o2m.quantize_fp8(b, (128, 128), R.E5M2 if m % 2 else E4M3, scales)
-    print("split", m, n, k, splits, scales, dtype, flush=True)
+    print("outputs", m, n, k, scales, dtype, flush=True)
     want = (R.values64(A, 1), R.values64(B, 128), dtype)
     C = o2m.gemm_fp8(A, B, dtype=dtype)
     R.check_product(C, *want)
@@ -160,6 +157,23 @@ def test_gemm_in_splits(o2m, m, n, k, splits, scales, dtype):  # noqa: F811
                 assert torch.equal(out.contiguous().view(torch.uint8), C.view(torch.uint8))   # NaN as well
             out.fill_(7.0)
             assert (buf == 7.0).all()
+
+
+@pytest.mark.parametrize("m,n,k,splits", SPLIT)
+@pytest.mark.parametrize("scales", ["pow2", "float32"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gemm_in_splits(o2m, m, n, k, splits, scales, dtype):  # noqa: F811
+    """Sums of splits joined."""
+    check_outputs(o2m, m, n, k, scales, dtype)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 77, 300), (5, 90, 300), (90, 31, 1041), (77, 150, 270), (1290, 1601, 97), (1800, 4090, 300),
+                                   (3700, 3601, 200)])
+@pytest.mark.parametrize("scales", ["pow2", "float32"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gemm_into_outputs(o2m, m, n, k, scales, dtype):  # noqa: F811
+    """The same for few rows on one side and for tiles of every size."""
+    check_outputs(o2m, m, n, k, scales, dtype)
 
 
 @pytest.mark.parametrize("tokens,n,k", SPLIT_LINEAR)
@@ -203,3 +217,61 @@ def test_gemm_of_cancelling_channels(o2m, m, n, k, scales):  # noqa: F811
     A, B = o2m.quantize_fp8(a, scales=scales), o2m.quantize_fp8(b, scales=scales)
     for dtype in TYPES:
         R.check_product(o2m.gemm_fp8(A, B, dtype=dtype), R.values64(A, 1), R.values64(B, 1), dtype)
+
+
+# ---- batches whose matrices lie side by side ---------------------------------------------
+
+@pytest.mark.parametrize("rows,cols", [(20, 33), (33, 20), (300, 200), (1, 50)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_updates_side_by_side(o2m, rows, cols, dtype):  # noqa: F811
+    """Heads that share their rows' memory, (rows, heads, cols) as (heads, rows, cols), in and out and in place."""
+    b = 5
+    g0 = torch.stack([matrix(rows, cols, 60 + i, dtype, spread=0.3) for i in range(b)])
+    want = o2m.orthogonalize(g0)
+    side = torch.full((rows + 1, b, cols + 3), 7.0, dtype=dtype, device=DEV)
+    out = side[:rows, :, :cols].transpose(0, 1)
+    assert o2m.orthogonalize(g0, out=out) is out
+    assert torch.equal(out, want)
+    out.copy_(g0)
+    assert torch.equal(o2m.orthogonalize(out), want)
+    assert torch.equal(o2m.orthogonalize(out, out=out), want)
+    out.fill_(7.0)
+    assert (side == 7.0).all()
+
+
+# ---- graphs and streams -------------------------------------------------------------------
+
+def test_graphs_of_a_training_step(o2m):  # noqa: F811
+    """Two captured training steps of layers whose products are split and whose updates take one launch and
+    several, replayed in turn with eager work between; each replay as the eager step on the same inputs."""
+    def step(x, w, dy, total):
+        xq, xt = o2m.quantize_fp8_pair(x)
+        wq, wt = o2m.quantize_fp8_pair(w, (128, 128))
+        y = o2m.gemm_fp8(xq, wq)
+        dx, dw = o2m.linear_fp8_backward(dy, xt, wt, dW=total, accumulate=True)
+        return y, o2m.linear_fp8(x[:1], wq), dx, dw, o2m.orthogonalize(dw)
+
+    shapes = [(8200, 65, 90), (70, 501, 4096)]   # tokens, n, k
+    side, graphs = torch.cuda.Stream(), []
+    for i, (t, n, k) in enumerate(shapes):
+        args = [torch.zeros((t, k), dtype=torch.bfloat16, device=DEV), torch.zeros((n, k), device=DEV),
+                torch.zeros((t, n), dtype=torch.bfloat16, device=DEV), torch.zeros((n, k), device=DEV)]
+        step(*args)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            out = step(*args)
+        graphs.append((g, args, out))
+    for seed in range(4):
+        want = []
+        for i, (g, args, _) in enumerate(graphs):
+            for j, a in enumerate(args):
+                a.copy_(matrix(*a.shape, 100 + 10 * seed + 5 * i + j, a.dtype, spread=0.3))
+            want.append([v.clone() for v in step(*args[:3], args[3].clone())])
+        torch.cuda.synchronize()
+        for g, *_ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for (_, _, out), ref in zip(graphs, want):
+            for a, b in zip(out, ref):
+                assert torch.equal(a, b), seed

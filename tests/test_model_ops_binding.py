@@ -197,3 +197,11 @@ def test_a_batch_of_small_updates_refuses_its_own_memory(dg, og, ldg, sg, do, oo
     coef = (ctypes.c_double * 3)(1.0, 1.0, 1.0)
     assert L.o2m_orthogonalize(2, 6, 9, ptr + 4 * dg, og, ldg, sg, ptr + 4 * do, oo, ldo, so, 0, 1,
                                ctypes.addressof(coef), 0.0, ptr, 256, None) == -8
+
+
+@pytest.mark.parametrize("oo,ldo,so", [(b"R", 17, 8), (b"R", 26, 9), (b"R", 27, 53), (b"C", 17, 6), (b"C", 62, 5)])
+def test_a_batch_refuses_results_that_share_entries(oo, ldo, so):
+    """3 matrices of 6 x 9 whose results meet, as rows side by side or one behind the other."""
+    ptr, coef = 1 << 20, (ctypes.c_double * 3)(1.0, 1.0, 1.0)
+    assert o2m._L.o2m_orthogonalize(3, 6, 9, ptr, b"R", 9, 54, 2 * ptr, oo, ldo, so, 0, 1, ctypes.addressof(coef), 0.0,
+                                    ptr, 256, None) == -11
