@@ -52,7 +52,8 @@ constexpr int kFewRows = 32;
 // 11.5 in 8; 64 x 4096 x 4096 (64) 16, and 10.7 in 4; 1000 x 1000 x 1000 (256) 6.9, and
 // 12.1 in 2.  (Near the edge the launch of its own that the joining takes decides:
 // 333 x 1283 x 2051 with 126 tiles takes the GPU 12.1 us, in 2 splits 10.8, but a linear
-// layer of it, launch by launch, 16 and 18.)
+// layer of it, launch by launch, 16 and 18.)  16 splits are the most, a bound that
+// no measurement set: 128 x 128 x 131072 takes 42 us in 16, on 64 workgroups.
 struct Fp8Plan {
     bool few;
     TileSize size;

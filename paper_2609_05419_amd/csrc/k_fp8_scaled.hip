@@ -1,6 +1,6 @@
 // 8-bit block-scaled products with power-of-two scales and 16-bit results: the
 // scaled MFMA applies them, so that nothing but MFMAs and the feeding of them is
-// left.  Large products take the pipeline of mfma_pipe.h (8192^3 391 us, 2.8
+// left.  Large products take the pipeline of mfma_pipe.h (8192^3 393 us, 2.8
 // PFLOP/s), 256 x 256 or 256 x 128, small ones tiles of 128 x 128
 // and 64 x 64.
 #include "fp8_tile.h"

@@ -512,6 +512,8 @@ struct ProductPlan {
 //   1024 x 8192, two parts, A    b/12 47, b/8 56, d/12 65;  X: c 62, b 64, d 93
 //   r = c = 1024, two parts, A   a/3 18, a'/6 16, b/4 18, a 29
 //   320 x 896, two parts, A      a/4 11, a 22, b/4 16
+// 16 splits are the most, a bound that no measurement set: an update of 128 x 131072
+// bf16 takes 377 us, with A in 48 workgroups.
 ProductPlan plan_product(int batch, int rows, int cols, int stages, bool sym) {
     struct Size {
         int tm, tn, resident;

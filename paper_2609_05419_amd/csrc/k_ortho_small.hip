@@ -6,7 +6,9 @@
 // its outputs (2 x 2 blocks of 16 x 16), between barriers; 15 of them for five
 // steps, where separate launches take 3 us and more each (16 matrices of 96 x 80
 // in fp32: 43 us, of them 14 to load and write and 5.8 a step, against 105 in 17
-// launches).
+// launches).  By count a step is some 2 us: 1024 threads leave a lane 128 registers, of
+// which 62 are spilled to scratch memory (28 with one part), and the k loop waits for
+// each of its LDS reads.
 #include "ortho_shared.h"
 
 #include <math.h>
