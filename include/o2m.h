@@ -276,7 +276,7 @@ o2m_status zgemm_2m_residues_ex(int m, int n, int k, const double *A, int lda, c
  * they may. Sizes past what a call's kernels cover are refused with O2M_ERR_SIZE:
  * rows, tokens, m and n reach 2^31 - 1024 at most, and a launch 2^32 - 1 threads,
  * which is below 2^28 blocks of 1 x 128 or 2^23 of 128 x 128 to be quantized, and
- * below 2^28 rows beside up to 32 of the other operand, some 2^29 beside up to 128.
+ * below 2^28 rows beside up to 32 of the other operand and 2^30 beside up to 64.
  * ------------------------------------------------------------------------ */
 
 /* element types of unquantized matrices */
