@@ -275,3 +275,53 @@ def test_graphs_of_a_training_step(o2m):  # noqa: F811
         for (_, _, out), ref in zip(graphs, want):
             for a, b in zip(out, ref):
                 assert torch.equal(a, b), seed
+
+
+# ---- the longest rows ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("m,n", [(3, 40), (40, 65), (2100, 2049)])
+@pytest.mark.parametrize("scales", ["pow2", "float32"])
+def test_gemm_of_the_longest_rows(o2m, m, n, scales):  # noqa: F811
+    """Rows of 2^23 - 16 values, the pitch at which offsets within a tile come closest to 2^31: row i holds
+    one power of two throughout, so every sum is exact and a result is rounded once."""
+    k = (1 << 23) - 16
+    code = torch.tensor([0x38, 0x30, 0x40, 0xB8], dtype=torch.uint8, device=DEV)      # 1, 1/2, 2, -1 in e4m3
+    value = torch.tensor([1.0, 0.5, 2.0, -1.0], dtype=torch.float64, device=DEV)
+
+    def operand(rows):
+        kind = (torch.arange(rows, device=DEV) * 7 // 3) % 4
+        q = torch.empty((rows, k), dtype=torch.uint8, device=DEV)
+        q.copy_(code[kind][:, None])
+        s = torch.full((-(-k // 128), rows), 127, dtype=torch.uint8, device=DEV) if scales == "pow2" else \
+            torch.ones((-(-k // 128), rows), device=DEV)
+        return (q.view(E4M3), s.t()), value[kind]
+    (A, a), (B, b) = operand(m), operand(n)
+    exact = k * a[:, None] * b[None, :]
+    for dtype in (torch.bfloat16, torch.float32):
+        print("longest", m, n, scales, dtype, flush=True)
+        C = o2m.gemm_fp8(A, B, dtype=dtype)
+        assert torch.equal(C, exact.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("r", [1, 256])
+def test_update_of_the_longest_rows(o2m, r, dtype):  # noqa: F811
+    """Rows of 2^21 entries, up to 2^29 in all, one per row not zero: X stays such a matrix, of the scalars
+    x <- a x + b x^3 + c x^5.  All sums have one term, so what is off is the roundings of held numbers,
+    u relative each (2^-11 in one fp16 part, 2^-21 in two), and of fp32, u / 8.  An error of x comes out of a step
+    multiplied by |p'| x / p; the step adds A's, by |b A + 2 c A^2| / |B|, B's, those of B's three terms, by the
+    largest one / |B| and 3 / 8, and X's.  One row: x is 1, 0.70, 1.11.  First step 1.03 + 1.02 + 1 + 2.6 + 1 = 6.7 u,
+    second 0.72 * 6.7 + 0.86 + 1 + 0.8 + 1 = 8.5 u, below 20.  256 rows: x is 1/16, 0.21, 0.69.  First 1 + 0.01 + 1 +
+    0.4 + 1 = 3.4 u, second 0.9 * 3.4 + 0.1 + 1 + 0.4 + 1 = 5.6 u, below 8.  Then the result's rounding."""
+    c = 1 << 21
+    u = 2.0 ** (-11 if dtype == torch.bfloat16 else -21)
+    g = torch.zeros((r, c), dtype=dtype, device=DEV)
+    g[:, 1000:1000 + r].diagonal().fill_(3.0)
+    x = o2m.orthogonalize(g, steps=2)
+    s = 1.0 / r ** 0.5
+    for _ in range(2):
+        s = R.COEF[0] * s + R.COEF[1] * s ** 3 + R.COEF[2] * s ** 5
+    d = x[:, 1000:1000 + r].diagonal()
+    assert (d.double() - s).abs().max().item() <= ((20 if r == 1 else 8) * u + R.half_step(dtype)) * abs(s)
+    d.zero_()
+    assert not x.any()
