@@ -244,8 +244,9 @@ struct HalfSrc {
         lo_a = (int)g.p.lo * 2;
         lo_b = (int)g.q.lo * 2;
         auto rows = [&](const Planes &of, int row0, int all, int tile, int ld, int lo) {
-            const int extent = lo + (min(tile, all - row0) - 1) * ld + kblocks * kStageRowBytes;
-            return __builtin_amdgcn_make_buffer_rsrc(of.hi + b * of.batch + row0 * of.pitch, (short)0, extent, 0x00020000);
+            // (2^31 at most, of 256 rows of 2^21 entries in two parts)
+            const uint32_t extent = (uint32_t)lo + (uint32_t)((min(tile, all - row0) - 1) * ld) + kblocks * kStageRowBytes;
+            return __builtin_amdgcn_make_buffer_rsrc(of.hi + b * of.batch + row0 * of.pitch, (short)0, (int)extent, 0x00020000);
         };
         rp = rows(g.p, i0, g.rows, tile_m, ld_a, SPLIT ? lo_a : 0);
         rq = rows(g.q, j0, g.cols, tile_n, ld_b, SPLIT ? lo_b : 0);
